@@ -44,7 +44,8 @@ enum {
   RESLIM_EWORKSPACE = -5  /* workspace missing, misaligned (256 B) or too small  */
 };
 
-enum { RESLIM_F32 = 0, RESLIM_BF16 = 1 };
+enum { RESLIM_F32 = 0, RESLIM_BF16 = 1,
+       RESLIM_E4M3 = 2 /* 8 bits: sign, 4 of exponent (bias 7), 3 of mantissa, no infinities; largest value 448.  Where stated only */ };
 
 /* Problem description.  Plain data, caller-owned, copied by reslim_create. */
 typedef struct {
@@ -127,7 +128,8 @@ int reslim_create(const reslim_config *cfg, const reslim_weights *w, reslim_ctx 
 void reslim_destroy(reslim_ctx *ctx);
 
 /* Text of the most recent error of `ctx`, or of the calling thread's last failed
- * reslim_create/tiles_partition when ctx is NULL.  Owned by the library. */
+ * reslim_create/tiles_partition/reslim_rmsnorm_... / reslim_rotary_... / reslim_gated_mlp_...
+ * when ctx is NULL.  Owned by the library. */
 const char *reslim_last_error(const reslim_ctx *ctx);
 
 /* n_h of the context's tiling (tile-major tokens per sample). */
@@ -563,6 +565,118 @@ int reslim_asc_block_bwd(reslim_ctx *ctx, const reslim_asc_plan *plan, int32_t l
  * a plan of another context. */
 int reslim_asc_forward(reslim_ctx *ctx, const reslim_asc_plan *plan, const float *x, float *y, void *workspace,
                        size_t ws_bytes, void *hip_stream);
+
+/* ---- Operators of gated pre-norm blocks, beside the model's own LayerNorm, attention and feed-forward kernels: a block
+ *   s = x + delta;  a = rmsnorm(s);  q | k | v = a W;  q, k = rotary(q, k);  delta = attention;
+ *   s = s + delta;  b = rmsnorm(s);  delta = gated_mlp(b)
+ * around tiles_attention_fwd, and its gradient.  No context is needed; sizes come with the call.  All pointers are device
+ * pointers on the current device unless stated; tensors are contiguous row-major unless a stride is given; work is enqueued
+ * on hip_stream, nothing is allocated or synchronised, and calls with buffers of their own may overlap.  Results are
+ * deterministic.  Sums, statistics and products are fp32 (angles 64-bit), results are rounded once.  rows = 0 (tokens = 0)
+ * is allowed: nothing is written but parameter gradients, which become zero.  A refusal enqueues nothing; its text is at
+ * reslim_last_error(NULL).  Errors: RESLIM_EINVAL (null, type, alignment, value), RESLIM_ESHAPE, RESLIM_EWORKSPACE (null,
+ * not 256-byte aligned, too small), RESLIM_EHIP. ---- */
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   s = x + delta (delta NULL: s = x);  y = s / sqrt(mean(s^2) + eps) * gamma;  sum = s.
+ *   x, sum  stream_dtype [rows, D]   the residual stream; sum may be x (in place) or NULL (not written)
+ *   delta   act_dtype [rows, D] or NULL
+ *   gamma   float [D]
+ *   y       y_dtype [rows, D]: act_dtype, or RESLIM_E4M3 with y_scale float [rows]: row i stands for y[i, :] * y_scale[i],
+ *           y_scale = max |.| of the row / 448 (a row of zeros has scale 0)
+ * (stream_dtype, act_dtype) = (F32, F32), (F32, BF16) or (BF16, BF16); 1 <= D <= 16384; eps >= 0.  s is normalised before it
+ * is rounded to the stream's type.  A value that is not finite stays in its row.  Buffers are aligned to their elements;
+ * rows of a multiple of 16 bytes of the stream that start on 16 bytes run at full speed, others element by element. */
+int reslim_rmsnorm_fwd(const void *x, const void *delta, const float *gamma, float eps, int64_t rows, int32_t D,
+                       int32_t stream_dtype, int32_t act_dtype, int32_t y_dtype, void *sum, void *y, float *y_scale,
+                       void *hip_stream);
+
+/* Its gradient: with g = gamma dy, r = 1 / sqrt(mean(s^2) + eps),
+ *   dx = d_sum + r (g - s r mean(g s r));  d_delta = dx;  dgamma = sum over rows of dy s r.
+ *   sum     stream_dtype [rows, D]  the forward's s (x where nothing was added)
+ *   dy      act_dtype [rows, D]
+ *   d_sum   stream_dtype [rows, D] or NULL: the gradient that reaches s past the norm
+ *   dx      stream_dtype [rows, D] out; may be d_sum (in place)
+ *   d_delta act_dtype [rows, D] out or NULL: the same gradient in delta's type
+ *   dgamma  float [D] out, written
+ *   workspace >= reslim_rmsnorm_bwd_workspace_bytes() */
+int reslim_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t D, size_t *out);
+int reslim_rmsnorm_bwd(const void *sum, const void *dy, const float *gamma, float eps, const void *d_sum, int64_t rows,
+                       int32_t D, int32_t stream_dtype, int32_t act_dtype, void *dx, void *d_delta, float *dgamma,
+                       void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Rotary positions.  The first `rot` features of a head are rot / 2 pairs, (2j, 2j + 1) or (j, j + rot / 2) by layout; pair j
+ * of token t turns by the angle positions[axis, t mod period] * freq[j] radians,
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos),
+ * axis = 0, or with axes = 2 (rows and columns of the patch grid) 1 in the second half of the pairs.  Features from `rot` on
+ * are copied.
+ *   x         dtype: token t's heads at t * x_stride elements, `heads` heads of dh features one after the other: the q and
+ *             k heads of [tokens, 3, heads, dh] are the first 2/3 (any number of heads that lie in front)
+ *   out       dtype, out_stride likewise; out == x with the same stride rotates in place; otherwise they must not overlap.
+ *             Only the `heads` rotated heads are written
+ *   positions int32 [axes, period];  freq double [rot / 2];  dtype RESLIM_F32 or RESLIM_BF16
+ * rot: a multiple of 2 * axes, at most dh; dh even, at most 1024; x_stride, out_stride >= heads * dh.  Interleaved bf16 pairs
+ * start on 4 bytes.  Full speed: pieces of 16 bytes that neither a head's start, rot (rot / 2 for pairs of halves) nor
+ * dh cuts; other sizes go pair by pair.
+ * reslim_rotary_bwd is the gradient, the same turn backwards: d_out in, d_x out (in place allowed). */
+enum { RESLIM_ROTARY_INTERLEAVED = 0, RESLIM_ROTARY_HALVES = 1 };
+int reslim_rotary_fwd(const void *x, void *out, const int32_t *positions, const double *freq, int64_t tokens, int64_t x_stride,
+                      int64_t out_stride, int64_t period, int32_t heads, int32_t dh, int32_t rot, int32_t axes, int32_t layout,
+                      float amplitude, int32_t dtype, void *hip_stream);
+int reslim_rotary_bwd(const void *d_out, void *d_x, const int32_t *positions, const double *freq, int64_t tokens,
+                      int64_t d_out_stride, int64_t d_x_stride, int64_t period, int32_t heads, int32_t dh, int32_t rot, int32_t axes,
+                      int32_t layout, float amplitude, int32_t dtype, void *hip_stream);
+
+/* HOST function: the frequency table of reslim_rotary_fwd, freq host double [rot / 2] out, *amplitude out.  With d = rot / axes
+ * features an axis, f_j = base^(-2 j / d), the same for either axis, and for contexts longer than the one trained on by `factor`:
+ *   PLAIN     f_j
+ *   LINEAR    f_j / factor                                       (positions interpolated)
+ *   BASE      with base * factor^(d / (d - 2)) for base          (the slowest pair is stretched by factor, the fastest not)
+ *   BY_PARTS  k f_j + (1 - k) f_j / factor, k = clamp((original_length f_j / 2 pi - 1) / 31, 0, 1): pairs that turn 32 times
+ *             and more over the original context stay, those that turn less than once are interpolated;
+ *             amplitude = 0.1 ln(factor) + 1 (1 elsewhere)
+ * factor >= 1 and original_length >= 1 where they are used. */
+enum { RESLIM_ROTARY_PLAIN = 0, RESLIM_ROTARY_LINEAR = 1, RESLIM_ROTARY_BASE = 2, RESLIM_ROTARY_BY_PARTS = 3 };
+int reslim_rotary_frequencies(int32_t rot, int32_t axes, double base, int32_t scaling, double factor, double original_length,
+                              double *freq, float *amplitude);
+
+/* Gated feed-forward layer:  [g | u] = x W_in^T + b_in,  h = act(g) o u,  y = h W_out^T + b_out,  act = SiLU or exact GELU.
+ *   w_in  x_dtype [2R, D], gate rows then up rows; with RESLIM_E4M3 row n stands for w_in[n, :] * in_scale[n], in_scale float [2R]
+ *   w_out act [D, R];  b_in float [2R], b_out float [D], either may be NULL
+ * Types: x_dtype F32 (act float), BF16 (act bfloat16) or E4M3 (act bfloat16; forward only): x rows with x_scale float [rows] as
+ * reslim_rmsnorm_fwd writes them.  D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
+ * sizes, rows <= 8,000,000.  BF16 and E4M3 buffers start on 16 bytes. */
+enum { RESLIM_GATE_SILU = 0, RESLIM_GATE_GELU = 1 };
+typedef struct {
+  const void *w_in;
+  const float *in_scale;    /* RESLIM_E4M3 only, else NULL */
+  const float *b_in;
+  const void *w_out;
+  const float *b_out;
+} reslim_gated_mlp_weights;
+
+/* y act [rows, D] from x x_dtype [rows, D] (x_scale: RESLIM_E4M3 only, else NULL).  The hidden layer is rounded to act
+ * between the two products.  y must not alias an input. */
+int reslim_gated_mlp_workspace_bytes(int32_t rows, int32_t D, int32_t R, int32_t x_dtype, size_t *out);
+int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const reslim_gated_mlp_weights *w, int32_t gate, int32_t rows,
+                         int32_t D, int32_t R, int32_t x_dtype, void *y, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* The same for training: also writes what the gradient reads, gu act [rows, 2R] = [g | u] and h act [rows, R].  x_dtype F32 or
+ * BF16. */
+int reslim_gated_mlp_fwd_train(const void *x, const reslim_gated_mlp_weights *w, int32_t gate, int32_t rows, int32_t D, int32_t R,
+                               int32_t x_dtype, void *gu, void *h, void *y, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Gradient:  dh = dy W_out,  dg = dh u act'(g),  du = dh act(g),  dx = [dg | du] W_in,  dW_in = [dg | du]^T x,  dW_out = dy^T h,
+ * biases: column sums of [dg | du] and dy.
+ *   x, gu, h as in the training forward; dy act [rows, D]; dx act [rows, D] out or NULL (skipped)
+ *   grads: w_in, w_out (out, shapes of the weights), b_in, b_out (out or NULL), all of grad_dtype: F32, or BF16 with x_dtype
+ *   BF16; written, not accumulated, summed over the rows in fp32 in a fixed order.
+ * [dg | du] is rounded to act between the products. */
+typedef struct { void *w_in, *b_in, *w_out, *b_out; } reslim_gated_mlp_grads;
+int reslim_gated_mlp_bwd_workspace_bytes(int32_t rows, int32_t D, int32_t R, int32_t x_dtype, int32_t grad_dtype, size_t *out);
+int reslim_gated_mlp_bwd(const void *x, const void *gu, const void *h, const void *dy, const reslim_gated_mlp_weights *w, int32_t gate,
+                         int32_t rows, int32_t D, int32_t R, int32_t x_dtype, int32_t grad_dtype, void *dx,
+                         const reslim_gated_mlp_grads *grads, void *workspace, size_t ws_bytes, void *hip_stream);
 
 /* Bandwidth yardstick: a plain device-to-device copy kernel (16 bytes per lane) of
  * `bytes` (a multiple of 16) from src to dst, both dev.  Profilers scale their HBM

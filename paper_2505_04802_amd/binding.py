@@ -16,7 +16,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libreslim.so")
 
 RESLIM_OK, RESLIM_EINVAL, RESLIM_ESHAPE, RESLIM_ENOMEM, RESLIM_EHIP, RESLIM_EWORKSPACE = 0, -1, -2, -3, -4, -5
-RESLIM_F32, RESLIM_BF16 = 0, 1
+RESLIM_F32, RESLIM_BF16, RESLIM_E4M3 = 0, 1, 2
+ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
+GATES = {"silu": 0, "gelu": 1}
 
 _CONFIG_FIELDS = ["in_vars", "out_vars", "H", "W", "scale", "patch", "embed_dim", "heads", "mlp_ratio",
                   "depth", "tiles_y", "tiles_x", "halo", "res_idx", "n_res", "dtype"]
@@ -43,7 +46,11 @@ EXPORTS = ["tiles_partition", "reslim_create", "reslim_destroy", "reslim_last_er
            "reslim_asc_build", "reslim_asc_build_tiles", "reslim_asc_edges", "reslim_asc_plan_create", "reslim_asc_plan_destroy",
            "reslim_asc_plan_info", "reslim_asc_image", "reslim_asc_compress", "reslim_asc_forward",
            "reslim_asc_decompress", "reslim_asc_compress_bwd", "reslim_asc_decompress_bwd",
-           "reslim_asc_block_train_bytes", "reslim_asc_block_fwd_train", "reslim_asc_block_bwd"]
+           "reslim_asc_block_train_bytes", "reslim_asc_block_fwd_train", "reslim_asc_block_bwd",
+           "reslim_rmsnorm_fwd", "reslim_rmsnorm_bwd_workspace_bytes", "reslim_rmsnorm_bwd",
+           "reslim_rotary_fwd", "reslim_rotary_bwd", "reslim_rotary_frequencies",
+           "reslim_gated_mlp_workspace_bytes", "reslim_gated_mlp_fwd", "reslim_gated_mlp_fwd_train",
+           "reslim_gated_mlp_bwd_workspace_bytes", "reslim_gated_mlp_bwd"]
 
 
 class ReslimConfigC(C.Structure):
@@ -72,6 +79,14 @@ MODEL_PARAMS = ("w_pe", "b_pe", "var_emb", "agg_q0", "agg_wq", "agg_bq", "agg_wk
 
 class GradsC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in MODEL_PARAMS]
+
+
+class GatedMlpWeightsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w_in", "in_scale", "b_in", "w_out", "b_out")]
+
+
+class GatedMlpGradsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w_in", "b_in", "w_out", "b_out")]
 
 
 class ProfileRecord(C.Structure):
@@ -161,6 +176,19 @@ def load() -> C.CDLL:
     lib.reslim_asc_block_train_bytes.argtypes = [vp, vp, szp, szp]
     lib.reslim_asc_block_fwd_train.argtypes = [vp, vp, i32, vp, vp, vp, C.c_size_t, vp, C.c_size_t, vp]
     lib.reslim_asc_block_bwd.argtypes = [vp, vp, i32, vp, vp, C.c_size_t, vp, vp, C.POINTER(BlockGradsC), vp, C.c_size_t, vp]
+    f32, i64 = C.c_float, C.c_int64
+    lib.reslim_rmsnorm_fwd.argtypes = [vp, vp, vp, f32, i64, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.reslim_rmsnorm_bwd_workspace_bytes.argtypes = [i64, i32, szp]
+    lib.reslim_rmsnorm_bwd.argtypes = [vp, vp, vp, f32, vp, i64, i32, i32, i32, vp, vp, vp, vp, C.c_size_t, vp]
+    for nm in ("reslim_rotary_fwd", "reslim_rotary_bwd"):
+        getattr(lib, nm).argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, i32, i32, f32, i32, vp]
+    lib.reslim_rotary_frequencies.argtypes = [i32, i32, C.c_double, i32, C.c_double, C.c_double, vp, C.POINTER(f32)]
+    gw, gg = C.POINTER(GatedMlpWeightsC), C.POINTER(GatedMlpGradsC)
+    lib.reslim_gated_mlp_workspace_bytes.argtypes = [i32, i32, i32, i32, szp]
+    lib.reslim_gated_mlp_fwd.argtypes = [vp, vp, gw, i32, i32, i32, i32, i32, vp, vp, C.c_size_t, vp]
+    lib.reslim_gated_mlp_fwd_train.argtypes = [vp, gw, i32, i32, i32, i32, i32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.reslim_gated_mlp_bwd_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, szp]
+    lib.reslim_gated_mlp_bwd.argtypes = [vp, vp, vp, vp, gw, i32, i32, i32, i32, i32, i32, vp, gg, vp, C.c_size_t, vp]
     lib.reslim_debug_set_gemm_tile.argtypes = [i32]
     lib.reslim_debug_set_gemm_tile.restype = None
     lib.reslim_debug_set_attention_variant.argtypes = [i32]
@@ -583,6 +611,177 @@ def reslim_asc_block_bwd(ctx, plan, layer, x_in, saved, d_x_out, d_x_in, grads, 
     _check(load().reslim_asc_block_bwd(ctx, plan, layer, x_in.data_ptr(), saved.data_ptr(), _nbytes(saved),
                                        d_x_out.data_ptr(), d_x_in.data_ptr(), C.byref(g), workspace.data_ptr(),
                                        _nbytes(workspace), _stream_ptr(stream)), ctx)
+
+
+# ------------------------------------------------------------------ operators of gated pre-norm blocks
+# These take no context.  Tensors are checked here (type, shape, contiguity, the current device), everything else in the library.
+_codes: Dict = {}
+
+
+def _code(dtype) -> int:
+    """RESLIM_F32, RESLIM_BF16 or RESLIM_E4M3 of a torch type."""
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: RESLIM_F32, torch.bfloat16: RESLIM_BF16, torch.float8_e4m3fn: RESLIM_E4M3})
+    if dtype not in _codes:
+        raise ValueError(f"type {dtype} is none of float32, bfloat16, float8_e4m3fn")
+    return _codes[dtype]
+
+
+def _fits(name: str, t, shape, dtype=None) -> int:
+    """The tensor's address, if it is a contiguous tensor of this shape (and type) on the current device."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)}: got {tuple(t.shape)}, strides {tuple(t.stride())}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}: got {t.dtype}")
+    return t.data_ptr()
+
+
+def _fits_or_none(name: str, t, shape, dtype=None):
+    return None if t is None else _fits(name, t, shape, dtype)
+
+
+def _room(workspace):
+    """(address, bytes) of a workspace, which may be None where none is needed."""
+    if workspace is None:
+        return None, 0
+    return _fits("workspace", workspace, workspace.shape), _nbytes(workspace)
+
+
+def reslim_rmsnorm_fwd(x, gamma, y, *, eps: float = 1e-6, delta=None, sum_out=None, y_scale=None, stream=None) -> None:
+    """y = rmsnorm(x + delta) * gamma and sum_out = x + delta (may be x).  x, sum_out [rows, D] fp32 or bf16; delta, y in the
+    activation type; y float8_e4m3fn with y_scale fp32 [rows]; gamma fp32 [D].  Without delta and with an 8-bit y the
+    activation type is the stream's."""
+    import torch
+    rows, D = x.shape
+    act = delta.dtype if delta is not None else x.dtype if y.dtype == torch.float8_e4m3fn else y.dtype
+    _check(load().reslim_rmsnorm_fwd(_fits("x", x, (rows, D)), _fits_or_none("delta", delta, (rows, D)), _fits("gamma", gamma, (D,), torch.float32),
+                                     eps, rows, D, _code(x.dtype), _code(act), _code(y.dtype), _fits_or_none("sum_out", sum_out, (rows, D), x.dtype),
+                                     _fits("y", y, (rows, D)), _fits_or_none("y_scale", y_scale, (rows,), torch.float32), _stream_ptr(stream)))
+
+
+def reslim_rmsnorm_bwd_workspace_bytes(rows: int, D: int) -> int:
+    n = C.c_size_t(0)
+    _check(load().reslim_rmsnorm_bwd_workspace_bytes(rows, D, C.byref(n)))
+    return n.value
+
+
+def reslim_rmsnorm_bwd(sum_in, dy, gamma, dx, dgamma, workspace, *, eps: float = 1e-6, d_sum=None, d_delta=None, stream=None) -> None:
+    """sum_in: the forward's x + delta; d_sum: the gradient that reaches it past the norm (may be dx); dx in the stream's type,
+    d_delta the same in dy's; dgamma fp32 [D]."""
+    import torch
+    rows, D = sum_in.shape
+    ws, n = _room(workspace)
+    _check(load().reslim_rmsnorm_bwd(_fits("sum_in", sum_in, (rows, D)), _fits("dy", dy, (rows, D)), _fits("gamma", gamma, (D,), torch.float32), eps,
+                                     _fits_or_none("d_sum", d_sum, (rows, D), sum_in.dtype), rows, D, _code(sum_in.dtype), _code(dy.dtype),
+                                     _fits("dx", dx, (rows, D), sum_in.dtype), _fits_or_none("d_delta", d_delta, (rows, D), dy.dtype),
+                                     _fits("dgamma", dgamma, (D,), torch.float32), ws, n, _stream_ptr(stream)))
+
+
+def reslim_rotary_frequencies(rot: int, axes: int = 1, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                              original_length: float = 1.0):
+    """Host function: (float64 [rot / 2] radians a position, factor on the rotated values)."""
+    freq = np.empty(max(rot, 2) // 2, np.float64)
+    amplitude = C.c_float(0.0)
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {tuple(ROTARY_SCALINGS)}")
+    _check(load().reslim_rotary_frequencies(rot, axes, base, ROTARY_SCALINGS[scaling], factor, original_length, freq.ctypes.data, C.byref(amplitude)))
+    return freq, float(amplitude.value)
+
+
+def _rotary(call, x, out, positions, freq, heads, layout, amplitude, stream):
+    import torch
+    if layout not in ROTARY_LAYOUTS:
+        raise ValueError(f"layout must be one of {tuple(ROTARY_LAYOUTS)}")
+    for name, t in (("x", x), ("out", out)):
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+        if t.dim() != 3 or t.shape[1] < heads or (t.shape[0] > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):
+            raise ValueError(f"{name} must be [tokens, at least {heads} heads, dh] with contiguous heads: got {tuple(t.shape)}, strides {tuple(t.stride())}")
+    tokens, _, dh = x.shape
+    if out.dtype != x.dtype or out.shape[0] != tokens or out.shape[2] != dh:
+        raise ValueError(f"out must match x in type, tokens and head size: {out.dtype} {tuple(out.shape)} for {x.dtype} {tuple(x.shape)}")
+    axes, period = positions.shape
+    # a dimension of one token may carry any stride
+    xs, os = (t.stride(0) if tokens > 1 else t.shape[1] * dh for t in (x, out))
+    _check(call(x.data_ptr(), out.data_ptr(), _fits("positions", positions, (axes, period), torch.int32), _fits("freq", freq, (freq.numel(),), torch.float64),
+                tokens, xs, os, period, heads, dh, 2 * freq.numel(), axes, ROTARY_LAYOUTS[layout], amplitude, _code(x.dtype), _stream_ptr(stream)))
+
+
+def reslim_rotary_fwd(x, out, positions, freq, *, heads: int, layout: str = "half", amplitude: float = 1.0, stream=None) -> None:
+    """The first `heads` heads of x [tokens, heads or more, dh] rotated by position into out (which may be x).  positions int32
+    [axes, period], token t taking column t mod period; freq float64 [rot / 2]; layout "half" or "interleaved"."""
+    _rotary(load().reslim_rotary_fwd, x, out, positions, freq, heads, layout, amplitude, stream)
+
+
+def reslim_rotary_bwd(d_out, d_x, positions, freq, *, heads: int, layout: str = "half", amplitude: float = 1.0, stream=None) -> None:
+    """The gradient of reslim_rotary_fwd: the same turn backwards; d_x may be d_out."""
+    _rotary(load().reslim_rotary_bwd, d_out, d_x, positions, freq, heads, layout, amplitude, stream)
+
+
+def _gate(gate: str) -> int:
+    if gate not in GATES:
+        raise ValueError(f"gate must be one of {tuple(GATES)}")
+    return GATES[gate]
+
+
+def _gated_weights(w, x, act):
+    """(struct, D, R) of the weights of a gated feed-forward layer: a dict of CUDA tensors w_in [2R, D] in x's type, w_out [D, R] in the
+    activations', and where present in_scale, b_in fp32 [2R], b_out fp32 [D]."""
+    import torch
+    D, R = w["w_out"].shape
+    return GatedMlpWeightsC(w_in=_fits("w_in", w["w_in"], (2 * R, D), x.dtype), in_scale=_fits_or_none("in_scale", w.get("in_scale"), (2 * R,), torch.float32),
+                            b_in=_fits_or_none("b_in", w.get("b_in"), (2 * R,), torch.float32), w_out=_fits("w_out", w["w_out"], (D, R), act),
+                            b_out=_fits_or_none("b_out", w.get("b_out"), (D,), torch.float32)), D, R
+
+
+def reslim_gated_mlp_workspace_bytes(rows: int, D: int, R: int, dtype) -> int:
+    """Workspace of reslim_gated_mlp_fwd and _fwd_train; dtype: x's torch type."""
+    n = C.c_size_t(0)
+    _check(load().reslim_gated_mlp_workspace_bytes(rows, D, R, _code(dtype), C.byref(n)))
+    return n.value
+
+
+def reslim_gated_mlp_fwd(x, weights, y, workspace, *, gate: str = "silu", x_scale=None, stream=None) -> None:
+    """y = (act(x Wg^T + bg) * (x Wu^T + bu)) Wo^T + bo; x [rows, D] fp32, bf16, or float8_e4m3fn with x_scale fp32 [rows]."""
+    import torch
+    act = torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype
+    w, D, R = _gated_weights(weights, x, act)
+    rows = x.shape[0]
+    ws, n = _room(workspace)
+    _check(load().reslim_gated_mlp_fwd(_fits("x", x, (rows, D)), _fits_or_none("x_scale", x_scale, (rows,), torch.float32), C.byref(w), _gate(gate),
+                                       rows, D, R, _code(x.dtype), _fits("y", y, (rows, D), act), ws, n, _stream_ptr(stream)))
+
+
+def reslim_gated_mlp_fwd_train(x, weights, gu, h, y, workspace, *, gate: str = "silu", stream=None) -> None:
+    """reslim_gated_mlp_fwd that also writes gu [rows, 2R] and h [rows, R], which reslim_gated_mlp_bwd reads."""
+    w, D, R = _gated_weights(weights, x, x.dtype)
+    rows = x.shape[0]
+    ws, n = _room(workspace)
+    _check(load().reslim_gated_mlp_fwd_train(_fits("x", x, (rows, D)), C.byref(w), _gate(gate), rows, D, R, _code(x.dtype),
+                                             _fits("gu", gu, (rows, 2 * R), x.dtype), _fits("h", h, (rows, R), x.dtype), _fits("y", y, (rows, D), x.dtype),
+                                             ws, n, _stream_ptr(stream)))
+
+
+def reslim_gated_mlp_bwd_workspace_bytes(rows: int, D: int, R: int, dtype, grad_dtype) -> int:
+    n = C.c_size_t(0)
+    _check(load().reslim_gated_mlp_bwd_workspace_bytes(rows, D, R, _code(dtype), _code(grad_dtype), C.byref(n)))
+    return n.value
+
+
+def reslim_gated_mlp_bwd(x, gu, h, dy, weights, dx, grads, workspace, *, gate: str = "silu", stream=None) -> None:
+    """grads: dict of CUDA tensors w_in, w_out and, where wanted, b_in, b_out, all fp32 or all bf16 (written); dx [rows, D] or None."""
+    w, D, R = _gated_weights(weights, x, x.dtype)
+    rows, gt = x.shape[0], grads["w_in"].dtype
+    g = GatedMlpGradsC(w_in=_fits("grads w_in", grads["w_in"], (2 * R, D), gt), b_in=_fits_or_none("grads b_in", grads.get("b_in"), (2 * R,), gt),
+                       w_out=_fits("grads w_out", grads["w_out"], (D, R), gt), b_out=_fits_or_none("grads b_out", grads.get("b_out"), (D,), gt))
+    ws, n = _room(workspace)
+    _check(load().reslim_gated_mlp_bwd(_fits("x", x, (rows, D)), _fits("gu", gu, (rows, 2 * R), x.dtype), _fits("h", h, (rows, R), x.dtype),
+                                       _fits("dy", dy, (rows, D), x.dtype), C.byref(w), _gate(gate), rows, D, R, _code(x.dtype), _code(gt),
+                                       _fits_or_none("dx", dx, (rows, D), x.dtype), C.byref(g), ws, n, _stream_ptr(stream)))
 
 
 # ------------------------------------------------------------------ convenience holder

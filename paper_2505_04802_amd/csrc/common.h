@@ -234,13 +234,16 @@ hipError_t attention_bwd_init();
 hipError_t wgrad_init();
 // parameter gradients of up to kWgradMax linear layers at once
 size_t wgrad_ws_bytes(int dtype, const WgradOp *op, int n_op, int M);
-hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st);
+size_t wgrad_rounded_ws_bytes(const WgradOp *op, int n_op, int M);
+hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded = false);
 int layernorm_bwd_slabs(int64_t rows);   // partial rows (of 2 D floats) launch_layernorm_bwd writes
 hipError_t launch_layernorm_bwd(int dtype, const float *x, const void *dy, const float *g, const float *res,
                                 float *dx_out, void *act_out, float *partial, float *dgamma, float *dbeta,
                                 int64_t rows, int D, hipStream_t st);
 hipError_t launch_gelu(int dtype, bool bwd, const void *h, const void *dy, void *out, int64_t n, hipStream_t st);
 hipError_t launch_to_act(int dtype, const float *src, void *dst, int64_t n, hipStream_t st);
+// out[j] = sum of partial[p * stride + j] over p < n_part in a fixed order (no partial rows: zeros)
+hipError_t launch_partial_reduce(const float *partial, float *out, int n_part, int64_t stride, int64_t n, hipStream_t st);
 int colsum_slabs(int64_t rows);          // partial rows (of N floats) launch_colsum writes
 hipError_t launch_colsum(const float *a, float *partial, float *out, int64_t rows, int N, hipStream_t st);
 hipError_t launch_transpose(int dtype, const void *src, void *dst, int R, int C, hipStream_t st);

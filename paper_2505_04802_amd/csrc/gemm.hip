@@ -18,40 +18,10 @@
 
 #include "common.h"
 #include "gelu.h"
-#include "gemm_cursor.h"
+#include "gemm_kernel.h"
 #include "gemm_plan.h"
 
 namespace reslim {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-
-struct GemmArgs {
-  const void *A;
-  const void *W;
-  const float *bias;
-  void *out;
-  const float *tab;
-  int ldo, tab_rows;
-  int M, N, K;
-  int grid_m, grid_n;
-  float qscale;   // EPI_BIAS_QSCALE_ACT: factor applied to output columns n < qcols
-  int qcols;
-  int col_fast;            // one-tile-per-work-group kernel: tile order inside a band
-  const void *aux;         // EPI_BIAS_RES_F32: skip input (fp32), layout of out unless res_map is set
-  const int32_t *res_map;  // EPI_BIAS_RES_F32, optional: output row b*res_out + r reads skip row b*res_in + res_map[r]
-  int res_out;
-  int64_t res_in;
-  void *out2;              // EPI_BIAS_ACT_GELU2: second output (act), layout of out
-  // fp32 kernel with LayerNorm in front: gain and bias; rows of A through a map (see ResRowMap) where it is set
-  const float *ln_g, *ln_b;
-  const int32_t *a_map;
-  int a_out;
-  int64_t a_in;
-};
-
 
 __device__ __forceinline__ float gelu_erf(float x) {
   return 0.5f * x * (1.0f + erff(x * 0.70710678118654752440f));
@@ -63,12 +33,6 @@ __device__ __forceinline__ float gelu_erf(float x) {
 // ones 32 rows x 64 columns at a time, fp32 ones 32 x 32, so that a store instruction
 // writes eight complete 128-byte row segments (16 bytes per lane) instead of 32 or 64
 // partial ones; no barrier is involved, the LDS operations of one wave execute in order.
-template <int EPI>
-__device__ __host__ constexpr bool epi_act_out() {
-  return EPI == EPI_BIAS_ACT || EPI == EPI_BIAS_QSCALE_ACT || EPI == EPI_BIAS_GELU_ACT || EPI == EPI_BIAS_ACT_GELU2;
-}
-constexpr int kEpiStageBytes = 4096;    // per wave
-
 // one value of a bf16-output epilogue (v already carries the bias); sc: the factor of the value's
 // block of 32 columns (EPI_BIAS_QSCALE_ACT: qcols is a multiple of 32, so a block is scaled as a
 // whole and the factor is one scalar per block, not a register per column)
@@ -231,161 +195,7 @@ __device__ __forceinline__ void epilogue_wave(const GemmArgs &g, const f32x16 (&
   else epilogue_f32<EPI, GUARD, MI, NI, EPI == EPI_BIAS_RES_F32 ? 2 : 3>(g, acc, m_base, n_base, lane, stg);
 }
 
-// tile id seen by the hardware dispatcher -> tile id in XCD-contiguous order
-__device__ __forceinline__ int xcd_remap(int pid, int total) {
-  constexpr int NXCD = 8;
-  const int x = pid % NXCD, local = pid / NXCD;
-  const int q = total / NXCD, r = total % NXCD;
-  return x * q + (x < r ? x : r) + local;
-}
-
-template <int BM, int BN, int BK, int WM, int WN, int NBUF, int MINW, int EPI>
-__global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_bf16_kernel(GemmArgs g) {
-  constexpr int NT = WM * WN * 64;
-  constexpr int PITCH = BK + 8;           // bf16 elements per LDS row
-  constexpr int TM = BM / WM, TN = BN / WN;
-  constexpr int MI = TM / 32, NI = TN / 32;
-  constexpr int KC = BK / 8;              // 16-byte chunks per slab row
-  constexpr int CA = BM * KC / NT, CB = BN * KC / NT;
-  static_assert(BM * KC % NT == 0 && BN * KC % NT == 0, "slab must split evenly over threads");
-  static_assert(TM % 32 == 0 && TN % 32 == 0 && BK % 16 == 0, "MFMA tiling");
-  constexpr int GROUP_M = 8;
-
-  extern __shared__ __align__(16) unsigned char smem[];
-  bf16_t *As = reinterpret_cast<bf16_t *>(smem);        // [NBUF][BM][PITCH]
-  bf16_t *Bs = As + NBUF * BM * PITCH;                   // [NBUF][BN][PITCH]
-
-  const int total = g.grid_m * g.grid_n;
-  int pid = xcd_remap(blockIdx.x, total);
-  const int band = GROUP_M * g.grid_n;
-  const int band_id = pid / band;
-  const int first_m = band_id * GROUP_M;
-  const int band_rows = min(g.grid_m - first_m, GROUP_M);
-  // inside a band: rows fastest by default; columns fastest (the tiles that share an
-  // A panel are consecutive work-groups) when the host asks for it
-  const int tile_m = g.col_fast ? first_m + (pid % band) / g.grid_n : first_m + (pid % band) % band_rows;
-  const int tile_n = g.col_fast ? (pid % band) % g.grid_n : (pid % band) / band_rows;
-  const int m0 = tile_m * BM, n0 = tile_n * BN;
-
-  const int t = threadIdx.x;
-  const int lane = t & 63, wave = t >> 6;
-  const int wm = wave / WN, wn = wave % WN;
-  const int l32 = lane & 31, hi = lane >> 5;
-
-  const bf16_t *A = static_cast<const bf16_t *>(g.A);
-  const bf16_t *W = static_cast<const bf16_t *>(g.W);
-  const int K = g.K;
-
-  // per-thread global source rows (clamped: rows past the edge read valid memory,
-  // their results are never stored)
-  const bf16_t *a_src[CA];
-  const bf16_t *b_src[CB];
-  int a_dst[CA], b_dst[CB];
-#pragma unroll
-  for (int i = 0; i < CA; ++i) {
-    const int c = t + i * NT, row = c / KC, kc = c % KC;
-    const int gm = min(m0 + row, g.M - 1);
-    a_src[i] = A + static_cast<size_t>(gm) * K + kc * 8;
-    a_dst[i] = row * PITCH + kc * 8;
-  }
-#pragma unroll
-  for (int i = 0; i < CB; ++i) {
-    const int c = t + i * NT, row = c / KC, kc = c % KC;
-    const int gn = min(n0 + row, g.N - 1);
-    b_src[i] = W + static_cast<size_t>(gn) * K + kc * 8;
-    b_dst[i] = row * PITCH + kc * 8;
-  }
-
-  u32x4 ra[CA], rb[CB];
-  auto load_global = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < CA; ++i) ra[i] = *reinterpret_cast<const u32x4 *>(a_src[i] + k0);
-#pragma unroll
-    for (int i = 0; i < CB; ++i) rb[i] = *reinterpret_cast<const u32x4 *>(b_src[i] + k0);
-  };
-  auto store_lds = [&](int buf) {
-    bf16_t *as = As + buf * BM * PITCH;
-    bf16_t *bs = Bs + buf * BN * PITCH;
-#pragma unroll
-    for (int i = 0; i < CA; ++i) *reinterpret_cast<u32x4 *>(as + a_dst[i]) = ra[i];
-#pragma unroll
-    for (int i = 0; i < CB; ++i) *reinterpret_cast<u32x4 *>(bs + b_dst[i]) = rb[i];
-  };
-
-  f32x16 acc[MI][NI];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
-  const int nk = K / BK;
-  load_global(0);
-  if constexpr (NBUF == 2) {
-    store_lds(0);
-    __syncthreads();
-  }
-
-  const int a_frag = (wm * TM + l32) * PITCH + hi * 8;
-  const int b_frag = (wn * TN + l32) * PITCH + hi * 8;
-
-  // NBUF == 2: one barrier per slab, the next slab is written to the other buffer
-  // after this one has been consumed.  NBUF == 1: half the LDS (two work-groups per
-  // CU overlap each other's barriers and epilogues); the slab is written between two
-  // barriers and the next one is already in flight in registers during the MFMAs.
-  for (int kt = 0; kt < nk; ++kt) {
-    const int buf = NBUF == 2 ? (kt & 1) : 0;
-    if constexpr (NBUF == 1) {
-      if (kt > 0) __syncthreads();
-      store_lds(0);
-      __syncthreads();
-    }
-    if (kt + 1 < nk) load_global((kt + 1) * BK);
-    const bf16_t *as = As + buf * BM * PITCH + a_frag;
-    const bf16_t *bs = Bs + buf * BN * PITCH + b_frag;
-    // register double-buffered fragments: reads of step kk+1 go out right after the
-    // first MFMA of step kk
-    bf16x8 af[2][MI], bfr[2][NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) af[0][i] = *reinterpret_cast<const bf16x8 *>(as + i * 32 * PITCH);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) bfr[0][j] = *reinterpret_cast<const bf16x8 *>(bs + j * 32 * PITCH);
-#pragma unroll
-    for (int kk = 0; kk < BK / 16; ++kk) {
-      const int cur = kk & 1, nxt = cur ^ 1;
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[cur][j], af[cur][i], acc[i][j], 0, 0, 0);   // operands swapped: the block is C^T
-          if (i == 0 && j == 0) {
-            __builtin_amdgcn_sched_barrier(0);
-            if (kk + 1 < BK / 16) {
-#pragma unroll
-              for (int i2 = 0; i2 < MI; ++i2)
-                af[nxt][i2] = *reinterpret_cast<const bf16x8 *>(as + i2 * 32 * PITCH + (kk + 1) * 16);
-#pragma unroll
-              for (int j2 = 0; j2 < NI; ++j2)
-                bfr[nxt][j2] = *reinterpret_cast<const bf16x8 *>(bs + j2 * 32 * PITCH + (kk + 1) * 16);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (NBUF == 2) {
-      if (kt + 1 < nk) store_lds(buf ^ 1);
-      __syncthreads();
-    }
-  }
-
-  const int me = m0 + wm * TM, ne = n0 + wn * TN;
-  unsigned char *stg = smem + NBUF * (BM + BN) * PITCH * sizeof(bf16_t) + wave * kEpiStageBytes;
-  if (me + TM <= g.M && ne + TN <= g.N) epilogue_wave<EPI, false, MI, NI>(g, acc, me, ne, lane, stg);
-  else epilogue_wave<EPI, true, MI, NI>(g, acc, me, ne, lane, stg);
-}
-
+#include "gemm_small.inc"
 #include "gemm_pp.inc"
 
 // ------------------------------------------------------------------ fp32 path
@@ -551,37 +361,6 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(GemmArgs g) {
 }
 
 // ------------------------------------------------------------------ launchers
-template <int BM, int BN, int BK, int WM, int WN, int NBUF, int MINW>
-struct TileCfg {
-  static constexpr int kBM = BM, kBN = BN, kBK = BK, kWM = WM, kWN = WN, kNBUF = NBUF, kMINW = MINW;
-  static constexpr int kThreads = WM * WN * 64;
-  // operand slabs + the epilogue's staging area of every wave
-  static constexpr size_t kLds = static_cast<size_t>(NBUF) * (BM + BN) * (BK + 8) * sizeof(bf16_t) + WM * WN * kEpiStageBytes;
-};
-
-template <class TC, int EPI>
-static hipError_t set_attr() {
-  return hipFuncSetAttribute(
-      reinterpret_cast<const void *>(&gemm_bf16_kernel<TC::kBM, TC::kBN, TC::kBK, TC::kWM, TC::kWN, TC::kNBUF, TC::kMINW, EPI>),
-      hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(TC::kLds));
-}
-
-template <class TC, int EPI>
-static hipError_t launch_bf16_tc(GemmArgs g, hipStream_t st) {
-  g.grid_m = (g.M + TC::kBM - 1) / TC::kBM;
-  g.grid_n = (g.N + TC::kBN - 1) / TC::kBN;
-  const int total = g.grid_m * g.grid_n;
-  // Narrow outputs (up to four column tiles): putting the tiles that share an A panel
-  // on consecutive work-groups keeps them in step, so the panel is fetched from HBM
-  // once (measured -4% on the N = 512 products of c1, +7% on the N = 2048 one).
-  if (g.grid_n <= 4) g.col_fast = 1;
-  gemm_bf16_kernel<TC::kBM, TC::kBN, TC::kBK, TC::kWM, TC::kWN, TC::kNBUF, TC::kMINW, EPI>
-      <<<dim3(total), dim3(TC::kThreads), TC::kLds, st>>>(g);
-  return hipGetLastError();
-}
-
-typedef TileCfg<128, 128, 64, 2, 2, 1, 3> TileSmall;   // 64x64 per wave, 36 KB LDS, 3 WG / CU
-
 static int g_col_fast = 0;
 static int g_gemm_tile_override = -1;   // test / tuning hook: 2 = 128x128 tiles, 3 / 4 = persistent 256x256 / 128x256
 

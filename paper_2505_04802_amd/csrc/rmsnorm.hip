@@ -1,0 +1,321 @@
+// Root-mean-square norm of token rows with the residual's addition in front, and its gradient.
+//
+//   s = x + delta,  r = 1 / sqrt(mean(s^2) + eps),  y = s r gamma                      (forward)
+//   g = gamma dy,   ds = d_sum + r (g - s r mean(g s r)),  dgamma = sum_rows dy s r     (gradient)
+//
+// Both move every element once and compute next to nothing, so memory bounds them: a row stays in the registers of the
+// threads that share it (a wave up to 1024 features, a work-group beyond) between the sums and the result, every load
+// of a row is issued before the first is used, and 16 bytes of the stream is what a thread takes at a time.  Sums are
+// fp32 in an order that depends on the row's width and alignment alone, so a row's result does not depend on the
+// others.  s is normalised before it is rounded to the stream's type.
+#include <type_traits>
+
+#include "rows_common.h"
+
+namespace reslim {
+
+struct NormArgs {
+  const void *x, *delta;
+  const float *gamma;
+  void *sum, *y;
+  float *y_scale;
+  float eps;
+  int64_t rows;
+  int D;
+};
+
+template <class S, class A, class Y, int V, int NT, int NC>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a) {
+  constexpr int RPB = NT < 256 ? 256 / NT : 1;
+  __shared__ float box[2][NT / 64];
+  const int t = threadIdx.x % NT;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / NT;
+  if (row >= a.rows) return;                 // whole waves, and only where no barrier follows (NT == 64)
+  const int64_t at = row * a.D;
+  const S *x = static_cast<const S *>(a.x) + at;
+  const A *d = static_cast<const A *>(a.delta) + at;
+  float v[NC][V], w[NC][V];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int k = (i * NT + t) * V;
+    if (k < a.D) {
+      Piece<S, V>::load(x + k, v[i]);
+      if (a.delta) Piece<A, V>::load(d + k, w[i]);
+    }
+  }
+  float sq = 0.f;
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int k = (i * NT + t) * V;
+    if (k < a.D) {
+      if (a.delta) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j] += w[i][j];
+        if (a.sum) Piece<S, V>::store(static_cast<S *>(a.sum) + at + k, v[i]);
+      } else if (a.sum) {
+        Piece<S, V>::store(static_cast<S *>(a.sum) + at + k, v[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sq = fmaf(v[i][j], v[i][j], sq);
+    }
+  }
+  const float r = rsqrtf(row_all<NT, false>(sq, box[0]) / static_cast<float>(a.D) + a.eps);
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int k = (i * NT + t) * V;
+    if (k < a.D) {
+      float g[V];
+      Piece<float, V>::load(a.gamma + k, g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        v[i][j] = v[i][j] * r * g[j];
+        top = fmaxf(top, fabsf(v[i][j]));
+      }
+      if constexpr (!std::is_same<Y, e4m3_t>::value) Piece<Y, V>::store(static_cast<Y *>(a.y) + at + k, v[i]);
+    }
+  }
+  if constexpr (std::is_same<Y, e4m3_t>::value) {
+    // the largest magnitude of the row becomes 448; a row of zeros keeps scale 0 and zeros
+    top = row_all<NT, true>(top, box[1]);
+    if (t == 0) a.y_scale[row] = top / kE4m3Max;
+    const float up = top > 0.f ? fminf(kE4m3Max / top, 3.402823466e+38f) : 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int k = (i * NT + t) * V;
+      if (k < a.D) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j] *= up;
+        Piece<e4m3_t, V>::store(static_cast<e4m3_t *>(a.y) + at + k, v[i]);
+      }
+    }
+  }
+}
+
+struct NormBwdArgs {
+  const void *s, *dy, *d_sum;
+  const float *gamma;
+  void *dx, *d_delta;
+  float *partial;        // [work-groups, D]
+  float eps;
+  int64_t rows, rows_per_wg;
+  int D;
+};
+
+// A work-group owns a run of rows and keeps its part of dgamma in registers.
+template <class S, class A, int V, int NT, int NC>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_bwd_kernel(NormBwdArgs a) {
+  constexpr int RPB = NT < 256 ? 256 / NT : 1;
+  __shared__ float box[4][NT / 64];
+  __shared__ float sm[RPB > 1 ? RPB : 1][RPB > 1 ? NT * NC * V : 1];
+  const int t = threadIdx.x % NT, part = threadIdx.x / NT;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.rows_per_wg;
+  const int64_t r1 = r0 + a.rows_per_wg < a.rows ? r0 + a.rows_per_wg : a.rows;
+  // element by element the gains are read again where they are used: sixteen of them do not fit beside the rest
+  constexpr bool kKeep = V > 1;
+  float gam[kKeep ? NC : 1][V], acc[NC][V];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int k = (i * NT + t) * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[i][j] = 0.f;
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) gam[i][j] = 0.f;
+      if (k < a.D) Piece<float, V>::load(a.gamma + k, gam[i]);
+    }
+  }
+  auto gain = [&](int i, int j) { return kKeep ? gam[kKeep ? i : 0][j] : a.gamma[(i * NT + t) * V + j]; };
+  const float inv_d = 1.0f / static_cast<float>(a.D);
+  int turn = 0;
+  for (int64_t row = r0 + part; row < r1; row += RPB, turn ^= 1) {
+    const int64_t at = row * a.D;
+    float s[NC][V], e[NC][V], z[NC][V];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int k = (i * NT + t) * V;
+      if (k < a.D) {
+        Piece<S, V>::load(static_cast<const S *>(a.s) + at + k, s[i]);
+        Piece<A, V>::load(static_cast<const A *>(a.dy) + at + k, e[i]);
+        if (a.d_sum) Piece<S, V>::load(static_cast<const S *>(a.d_sum) + at + k, z[i]);
+      }
+    }
+    float sq = 0.f, gs = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if ((i * NT + t) * V < a.D) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          sq = fmaf(s[i][j], s[i][j], sq);
+          gs = fmaf(gain(i, j) * e[i][j], s[i][j], gs);
+        }
+      }
+    sq = row_all<NT, false>(sq, box[2 * turn]);
+    gs = row_all<NT, false>(gs, box[2 * turn + 1]);
+    const float r = rsqrtf(sq / static_cast<float>(a.D) + a.eps);
+    const float c = gs * r * inv_d;          // mean(g s r)
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int k = (i * NT + t) * V;
+      if (k < a.D) {
+        float o[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float h = s[i][j] * r;
+          acc[i][j] = fmaf(e[i][j], h, acc[i][j]);
+          o[j] = r * (gain(i, j) * e[i][j] - h * c);
+          if (a.d_sum) o[j] += z[i][j];
+        }
+        Piece<S, V>::store(static_cast<S *>(a.dx) + at + k, o);
+        if (a.d_delta) Piece<A, V>::store(static_cast<A *>(a.d_delta) + at + k, o);
+      }
+    }
+  }
+  float *out = a.partial + static_cast<int64_t>(blockIdx.x) * a.D;
+  if constexpr (RPB > 1) {                   // the row groups' sums, added in their order
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sm[part][(i * NT + t) * V + j] = acc[i][j];
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.D; k += 256) {
+      float v = sm[0][k];
+#pragma unroll
+      for (int p = 1; p < RPB; ++p) v += sm[p][k];
+      out[k] = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int k = (i * NT + t) * V;
+      if (k < a.D) Piece<float, V>::store(out + k, acc[i]);
+    }
+  }
+}
+
+constexpr int kNormMaxD = 16384;
+constexpr int kNormBwdGroups = 1024;      // four work-groups of 256 threads for every compute unit
+
+static int64_t norm_bwd_groups(int64_t rows) { return rows < kNormBwdGroups ? rows : kNormBwdGroups; }
+
+// Threads that share a row of D features and pieces of V that each holds: a wave, four or sixteen, with up to 16 features a thread
+// (the gradient keeps five values for each).
+template <int V, class F>
+static void norm_shape(int D, F &&f) {
+  using std::integral_constant;
+  auto fits = [&](auto nt, auto nc) {
+    if (D > decltype(nt)::value * decltype(nc)::value * V) return false;
+    f(nt, nc);
+    return true;
+  };
+  typedef integral_constant<int, 64> Wave;
+  typedef integral_constant<int, 256> Four;
+  typedef integral_constant<int, 1024> Sixteen;
+  typedef integral_constant<int, 16 / V> Full;
+  typedef integral_constant<int, V == 1 ? 4 : 8 / V> Part;
+  (void)(fits(Wave{}, integral_constant<int, 1>{}) || fits(Wave{}, Part{}) || fits(Wave{}, Full{}) || fits(Four{}, Part{}) || fits(Four{}, Full{}) ||
+         fits(Sixteen{}, Part{}) || fits(Sixteen{}, Full{}));
+}
+
+template <class S, class A, class Y, int V>
+static hipError_t launch_norm_v(const NormArgs &a, hipStream_t st) {
+  norm_shape<V>(a.D, [&](auto nt, auto nc) {
+    constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value, RPB = NT < 256 ? 256 / NT : 1;
+    rmsnorm_kernel<S, A, Y, V, NT, NC><<<dim3(static_cast<unsigned>((a.rows + RPB - 1) / RPB)), dim3(NT < 256 ? 256 : NT), 0, st>>>(a);
+  });
+  return hipGetLastError();
+}
+// whole pieces of 16 bytes of the stream where rows are made of them and start on them, else element by element
+template <class S, class A, class Y>
+static hipError_t launch_norm(const NormArgs &a, hipStream_t st) {
+  constexpr int V = 16 / sizeof(S);
+  const bool whole = a.D % V == 0 && aligned(a.x, 16) && aligned(a.sum, 16) && aligned(a.delta, V * sizeof(A)) && aligned(a.y, V * sizeof(Y)) && aligned(a.gamma, 16);
+  return whole ? launch_norm_v<S, A, Y, V>(a, st) : launch_norm_v<S, A, Y, 1>(a, st);
+}
+
+template <class S, class A, int V>
+static hipError_t launch_norm_bwd_v(NormBwdArgs a, float *dgamma, hipStream_t st) {
+  int64_t groups = norm_bwd_groups(a.rows);
+  if (groups > 0) {
+    a.rows_per_wg = (a.rows + groups - 1) / groups;
+    groups = (a.rows + a.rows_per_wg - 1) / a.rows_per_wg;
+    if (groups == 1) a.partial = dgamma;
+    norm_shape<V>(a.D, [&](auto nt, auto nc) {
+      constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value;
+      rmsnorm_bwd_kernel<S, A, V, NT, NC><<<dim3(static_cast<unsigned>(groups)), dim3(NT < 256 ? 256 : NT), 0, st>>>(a);
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || groups == 1) return e;
+  }
+  return launch_partial_reduce(a.partial, dgamma, static_cast<int>(groups), a.D, a.D, st);      // no rows: zeros
+}
+template <class S, class A>
+static hipError_t launch_norm_bwd(const NormBwdArgs &a, float *dgamma, hipStream_t st) {
+  constexpr int V = 16 / sizeof(S);
+  const bool whole = a.D % V == 0 && aligned(a.s, 16) && aligned(a.d_sum, 16) && aligned(a.dx, 16) && aligned(a.dy, V * sizeof(A)) &&
+                     aligned(a.d_delta, V * sizeof(A)) && aligned(a.gamma, 16) && aligned(dgamma, 16);
+  return whole ? launch_norm_bwd_v<S, A, V>(a, dgamma, st) : launch_norm_bwd_v<S, A, 1>(a, dgamma, st);
+}
+
+static int norm_check(const char *fn, int64_t rows, int D, float eps, int stream_dtype, int act_dtype) {
+  if (rows < 0 || rows > INT32_MAX || D < 1 || D > kNormMaxD) return refuse(RESLIM_ESHAPE, fn, "need 0 <= rows < 2^31 and 1 <= D <= 16384");
+  if (!(eps >= 0.f) || eps > 3.402823466e+38f) return refuse(RESLIM_EINVAL, fn, "eps must be finite and not negative");
+  const bool types = (stream_dtype == RESLIM_F32 && (act_dtype == RESLIM_F32 || act_dtype == RESLIM_BF16)) || (stream_dtype == RESLIM_BF16 && act_dtype == RESLIM_BF16);
+  return types ? RESLIM_OK : refuse(RESLIM_EINVAL, fn, "types must be (stream, act) = (F32, F32), (F32, BF16) or (BF16, BF16)");
+}
+
+}  // namespace reslim
+
+using namespace reslim;
+
+extern "C" int reslim_rmsnorm_fwd(const void *x, const void *delta, const float *gamma, float eps, int64_t rows, int32_t D, int32_t stream_dtype,
+                                  int32_t act_dtype, int32_t y_dtype, void *sum, void *y, float *y_scale, void *hip_stream) {
+  const char *fn = "reslim_rmsnorm_fwd";
+  const int rc = norm_check(fn, rows, D, eps, stream_dtype, act_dtype);
+  if (rc != RESLIM_OK) return rc;
+  if (y_dtype != act_dtype && y_dtype != RESLIM_E4M3) return refuse(RESLIM_EINVAL, fn, "y must have the activation type or be E4M3");
+  if ((y_dtype == RESLIM_E4M3) != (y_scale != nullptr)) return refuse(RESLIM_EINVAL, fn, "y_scale goes with E4M3 output, and only with it");
+  if (!gamma || (rows > 0 && (!x || !y))) return refuse(RESLIM_EINVAL, fn, "null buffer");
+  const size_t es = type_bytes(stream_dtype), ea = type_bytes(act_dtype);
+  if (!aligned(x, es) || !aligned(sum, es) || !aligned(delta, ea) || !aligned(y, type_bytes(y_dtype)) || !aligned(gamma, 4) || !aligned(y_scale, 4))
+    return refuse(RESLIM_EINVAL, fn, "a buffer is not aligned to its elements");
+  if (rows == 0) return RESLIM_OK;
+  const NormArgs a = {x, delta, gamma, sum, y, y_scale, eps, rows, D};
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  hipError_t e;
+  const bool q = y_dtype == RESLIM_E4M3;
+  if (stream_dtype == RESLIM_BF16) e = q ? launch_norm<bf16_t, bf16_t, e4m3_t>(a, st) : launch_norm<bf16_t, bf16_t, bf16_t>(a, st);
+  else if (act_dtype == RESLIM_BF16) e = q ? launch_norm<float, bf16_t, e4m3_t>(a, st) : launch_norm<float, bf16_t, bf16_t>(a, st);
+  else e = q ? launch_norm<float, float, e4m3_t>(a, st) : launch_norm<float, float, float>(a, st);
+  return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
+}
+
+extern "C" int reslim_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t D, size_t *out) {
+  const char *fn = "reslim_rmsnorm_bwd_workspace_bytes";
+  if (!out) return refuse(RESLIM_EINVAL, fn, "null argument");
+  const int rc = norm_check(fn, rows, D, 0.f, RESLIM_F32, RESLIM_F32);
+  if (rc != RESLIM_OK) return rc;
+  *out = align256(static_cast<size_t>(norm_bwd_groups(rows)) * D * sizeof(float));
+  return RESLIM_OK;
+}
+
+extern "C" int reslim_rmsnorm_bwd(const void *sum, const void *dy, const float *gamma, float eps, const void *d_sum, int64_t rows, int32_t D,
+                                  int32_t stream_dtype, int32_t act_dtype, void *dx, void *d_delta, float *dgamma, void *workspace,
+                                  size_t ws_bytes, void *hip_stream) {
+  const char *fn = "reslim_rmsnorm_bwd";
+  const int rc = norm_check(fn, rows, D, eps, stream_dtype, act_dtype);
+  if (rc != RESLIM_OK) return rc;
+  if (!gamma || !dgamma || (rows > 0 && (!sum || !dy || !dx))) return refuse(RESLIM_EINVAL, fn, "null buffer");
+  const size_t es = type_bytes(stream_dtype), ea = type_bytes(act_dtype);
+  if (!aligned(sum, es) || !aligned(d_sum, es) || !aligned(dx, es) || !aligned(dy, ea) || !aligned(d_delta, ea) || !aligned(gamma, 4) || !aligned(dgamma, 4))
+    return refuse(RESLIM_EINVAL, fn, "a buffer is not aligned to its elements");
+  if (rows > 1 && (!workspace || !aligned(workspace, 256) || ws_bytes < align256(static_cast<size_t>(norm_bwd_groups(rows)) * D * sizeof(float))))
+    return refuse(RESLIM_EWORKSPACE, fn, "workspace null, not 256-byte aligned or smaller than reslim_rmsnorm_bwd_workspace_bytes()");
+  const NormBwdArgs a = {sum, dy, d_sum, gamma, dx, d_delta, static_cast<float *>(workspace), eps, rows, 0, D};
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  hipError_t e;
+  if (stream_dtype == RESLIM_BF16) e = launch_norm_bwd<bf16_t, bf16_t>(a, dgamma, st);
+  else if (act_dtype == RESLIM_BF16) e = launch_norm_bwd<float, bf16_t>(a, dgamma, st);
+  else e = launch_norm_bwd<float, float>(a, dgamma, st);
+  return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
+}

@@ -1,0 +1,123 @@
+// Pieces shared by the kernels that work on rows in memory (rmsnorm.hip, rotary.hip): V consecutive elements of a row as
+// floats, sums and maxima over the threads that share a row, and the refusals of entry points that take no context.
+#pragma once
+
+#include <string>
+
+#include "common.h"
+
+namespace reslim {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_row;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_row;
+
+struct e4m3_t { uint8_t bits; };      // sign, 4 bits of exponent (bias 7), 3 of mantissa; largest 448, no infinities
+constexpr float kE4m3Max = 448.0f;
+
+// four floats to e4m3, to nearest, ties to even
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
+}
+
+// V consecutive elements; V > 1: the address is a multiple of V elements' bytes (at most 16)
+template <class T, int V> struct Piece;
+template <int V> struct Piece<float, V> {
+  static __device__ __forceinline__ void load(const float *p, float (&v)[V]) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(p + i);
+        v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = p[i];
+    }
+  }
+  static __device__ __forceinline__ void store(float *p, const float (&v)[V]) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = v[i];
+    }
+  }
+};
+template <int V> struct Piece<bf16_t, V> {
+  static __device__ __forceinline__ void load(const bf16_t *p, float (&v)[V]) {
+    uint32_t w[(V + 1) / 2];
+    if constexpr (V == 8) {
+      const u32x4_row r = *reinterpret_cast<const u32x4_row *>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = r[i];
+    } else if constexpr (V == 4) {
+      const u32x2_row r = *reinterpret_cast<const u32x2_row *>(p);
+      w[0] = r[0]; w[1] = r[1];
+    } else if constexpr (V == 2) {
+      w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else {
+      w[0] = *p;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  static __device__ __forceinline__ void store(bf16_t *p, const float (&v)[V]) {
+    if constexpr (V == 8) {
+      *reinterpret_cast<u32x4_row *>(p) = u32x4_row{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<u32x2_row *>(p) = u32x2_row{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    } else if constexpr (V == 2) {
+      *reinterpret_cast<uint32_t *>(p) = pack_bf16x2(v[0], v[1]);
+    } else {
+      *p = f32_to_bf16(v[0]);
+    }
+  }
+};
+template <int V> struct Piece<e4m3_t, V> {
+  static __device__ __forceinline__ void store(e4m3_t *p, const float (&v)[V]) {
+    if constexpr (V == 8) {
+      *reinterpret_cast<u32x2_row *>(p) = u32x2_row{pack_e4m3x4(v[0], v[1], v[2], v[3]), pack_e4m3x4(v[4], v[5], v[6], v[7])};
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<uint32_t *>(p) = pack_e4m3x4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i].bits = static_cast<uint8_t>(pack_e4m3x4(v[i], 0.f, 0.f, 0.f) & 0xff);
+    }
+  }
+};
+
+// Sum (or maximum) over the NT threads that share a row, the same value in all of them.  box: NT / 64 floats of LDS that nothing
+// else uses until every thread is past the call after next (two boxes taken in turn).
+template <int NT, bool MAX>
+__device__ __forceinline__ float row_all(float s, float *box) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const float o = __shfl_xor(s, m);
+    s = MAX ? fmaxf(s, o) : s + o;
+  }
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = box[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) s = MAX ? fmaxf(s, box[w]) : s + box[w];
+  }
+  return s;
+}
+
+// An entry point without a context refuses: the text goes to reslim_last_error(NULL).  Throws nothing.
+inline int refuse(int code, const char *fn, const char *why) noexcept {
+  try {
+    set_thread_error(std::string(fn) + ": " + why);
+  } catch (...) {
+  }
+  return code;
+}
+inline int refuse_hip(const char *fn, hipError_t e) noexcept { return refuse(RESLIM_EHIP, fn, hipGetErrorString(e)); }
+
+inline bool aligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+inline size_t type_bytes(int dtype) { return dtype == RESLIM_F32 ? 4 : dtype == RESLIM_BF16 ? 2 : 1; }
+
+}  // namespace reslim

@@ -399,10 +399,10 @@ static WgradPlan wgrad_plan(const WgradOp *op, int n_op, int M) { return wgrad_p
 struct WgradReduceArgs {
   const float4 *partial;
   int64_t stride4, end4[2 * kWgradMax];
-  float *out[2 * kWgradMax];
+  void *out[2 * kWgradMax];
   int n_part;
 };
-template <int G>
+template <int G, class T>
 __global__ __launch_bounds__(256) void wgrad_reduce_kernel(WgradReduceArgs a) {
   constexpr int COLS = 256 / G;
   __shared__ float4 sm[G > 1 ? 256 : 1];
@@ -435,16 +435,22 @@ __global__ __launch_bounds__(256) void wgrad_reduce_kernel(WgradReduceArgs a) {
   }
   if (j >= a.stride4) return;
   int64_t begin = 0;
-  float *out = a.out[0];
+  void *first = a.out[0];
 #pragma unroll
   for (int i = 1; i < 2 * kWgradMax; ++i) {
     const bool in = j >= a.end4[i - 1];
     begin = in ? +a.end4[i - 1] : +begin;
-    out = in ? +a.out[i] : +out;
+    first = in ? +a.out[i] : +first;
   }
-  out += 4 * (j - begin);
-  if ((reinterpret_cast<uintptr_t>(out) & 15) == 0) *reinterpret_cast<float4 *>(out) = acc;
-  else { out[0] = acc.x; out[1] = acc.y; out[2] = acc.z; out[3] = acc.w; }
+  T *out = static_cast<T *>(first) + 4 * (j - begin);
+  if constexpr (std::is_same<T, float>::value) {
+    if ((reinterpret_cast<uintptr_t>(out) & 15) == 0) *reinterpret_cast<float4 *>(out) = acc;
+    else { out[0] = acc.x; out[1] = acc.y; out[2] = acc.z; out[3] = acc.w; }
+  } else {                                   // gradients of the weights' own type, rounded once here
+    const u32x2 v = {pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+    if ((reinterpret_cast<uintptr_t>(out) & 7) == 0) *reinterpret_cast<u32x2 *>(out) = v;
+    else { out[0] = f32_to_bf16(acc.x); out[1] = f32_to_bf16(acc.y); out[2] = f32_to_bf16(acc.z); out[3] = f32_to_bf16(acc.w); }
+  }
 }
 
 // bytes of scratch the gradients of these layers need (0: none)
@@ -458,8 +464,14 @@ size_t wgrad_ws_bytes(int dtype, const WgradOp *op, int n_op, int M) {
   return p.splits > 1 ? align256(static_cast<size_t>(p.splits) * wgrad_slice(op, n_op) * sizeof(float)) : 0;
 }
 
-static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st) {
-  if (p.splits > 1 && !ws) return hipErrorInvalidValue;
+size_t wgrad_rounded_ws_bytes(const WgradOp *op, int n_op, int M) {
+  return align256(static_cast<size_t>(wgrad_plan(op, n_op, M).splits) * wgrad_slice(op, n_op) * sizeof(float));
+}
+
+// rounded: the gradients are bf16 (dw and db point at bf16), written by the sum over the slices, also of a single one
+static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded) {
+  const bool summed = rounded || p.splits > 1;
+  if (summed && !ws) return hipErrorInvalidValue;
   WgradArgs a = {};
   WgradReduceArgs r = {};
   for (int i = 0; i < kWgradMax; ++i) a.end[i] = INT32_MAX;
@@ -471,8 +483,8 @@ static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n
     const int64_t n_w = static_cast<int64_t>(op[i].N) * op[i].K;
     a.dy[i] = static_cast<const bf16_t *>(op[i].dy);
     a.x[i] = static_cast<const bf16_t *>(op[i].x);
-    a.out[i] = p.splits > 1 ? part + at : op[i].dw;
-    a.out_b[i] = p.splits > 1 ? part + at + n_w : op[i].db;
+    a.out[i] = summed ? part + at : op[i].dw;
+    a.out_b[i] = summed ? part + at + n_w : op[i].db;
     a.N[i] = op[i].N;
     a.K[i] = op[i].K;
     a.tiles_n[i] = wgrad_tiles_n(p.kind, a.N[i]);
@@ -492,24 +504,29 @@ static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n
   if (p.kind == kWgrad256) wgrad_bf16_kernel<2><<<grid, dim3(512), wgrad_lds<2>(), st>>>(a);
   else wgrad_bf16_kernel<1><<<grid, dim3(512), wgrad_lds<1>(), st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
+  if (e != hipSuccess || !summed) return e;
   r.partial = static_cast<const float4 *>(ws);
   r.stride4 = at / 4;
   r.n_part = p.splits;
   // small gradients have many slices: four groups of threads share them, or too few loads are in flight
-  if (p.splits >= 16) wgrad_reduce_kernel<4><<<dim3(static_cast<unsigned>((r.stride4 + 63) / 64)), dim3(256), 0, st>>>(r);
-  else wgrad_reduce_kernel<1><<<dim3(static_cast<unsigned>((r.stride4 + 255) / 256)), dim3(256), 0, st>>>(r);
+  const dim3 by4(static_cast<unsigned>((r.stride4 + 63) / 64)), by1(static_cast<unsigned>((r.stride4 + 255) / 256));
+  if (p.splits >= 16 && rounded) wgrad_reduce_kernel<4, bf16_t><<<by4, dim3(256), 0, st>>>(r);
+  else if (p.splits >= 16) wgrad_reduce_kernel<4, float><<<by4, dim3(256), 0, st>>>(r);
+  else if (rounded) wgrad_reduce_kernel<1, bf16_t><<<by1, dim3(256), 0, st>>>(r);
+  else wgrad_reduce_kernel<1, float><<<by1, dim3(256), 0, st>>>(r);
   return hipGetLastError();
 }
 
 // for each layer dW[N, K] = dY[M, N]^T X[M, K] and db[N] = column sums of dY, both fp32; ws as sized by wgrad_ws_bytes
-hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st) {
+// (rounded: bf16 operands, gradients rounded to bf16; ws as sized by wgrad_rounded_ws_bytes)
+hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded) {
+  if (rounded && dtype != RESLIM_BF16) return hipErrorInvalidValue;
   if (M <= 0 || n_op < 1 || n_op > kWgradMax) return hipErrorInvalidValue;
   for (int i = 0; i < n_op; ++i) {
     if (op[i].N <= 0 || op[i].K <= 0) return hipErrorInvalidValue;
     if (dtype == RESLIM_BF16 && (op[i].N % 8 != 0 || op[i].K % 8 != 0)) return hipErrorInvalidValue;
   }
-  if (dtype == RESLIM_BF16) return launch_wgrad_bf16(wgrad_plan(op, n_op, M), op, n_op, M, ws, st);
+  if (dtype == RESLIM_BF16) return launch_wgrad_bf16(wgrad_plan(op, n_op, M), op, n_op, M, ws, st, rounded);
   for (int i = 0; i < n_op; ++i) {
     const int64_t n = static_cast<int64_t>(op[i].N) * op[i].K;
     wgrad_f32_kernel<<<dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st>>>(
