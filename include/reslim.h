@@ -645,7 +645,7 @@ int reslim_rotary_frequencies(int32_t rot, int32_t axes, double base, int32_t sc
  *   w_out act [D, R];  b_in float [2R], b_out float [D], either may be NULL
  * Types: x_dtype F32 (act float), BF16 (act bfloat16) or E4M3 (act bfloat16; forward only): x rows with x_scale float [rows] as
  * reslim_rmsnorm_fwd writes them.  D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
- * sizes, rows <= 8,000,000.  BF16 and E4M3 buffers start on 16 bytes. */
+ * sizes, rows <= 4,000,000.  BF16 and E4M3 buffers start on 16 bytes. */
 enum { RESLIM_GATE_SILU = 0, RESLIM_GATE_GELU = 1 };
 typedef struct {
   const void *w_in;

@@ -623,32 +623,54 @@ def _code(dtype) -> int:
     if not _codes:
         import torch
         _codes.update({torch.float32: RESLIM_F32, torch.bfloat16: RESLIM_BF16, torch.float8_e4m3fn: RESLIM_E4M3})
-    if dtype not in _codes:
+    code = _codes.get(dtype)
+    if code is None:
         raise ValueError(f"type {dtype} is none of float32, bfloat16, float8_e4m3fn")
-    return _codes[dtype]
+    return code
 
 
-def _fits(name: str, t, shape, dtype=None) -> int:
-    """The tensor's address, if it is a contiguous tensor of this shape (and type) on the current device."""
+def _here():
+    """(current device, handle of its current stream).  torch.cuda.current_stream() makes an object of it, 2.7 us of a single token's
+    8.8; the accessor behind it takes 0.06."""
     import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)}: got {tuple(t.shape)}, strides {tuple(t.stride())}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}: got {t.dtype}")
+    dev = torch.cuda.current_device()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return dev, raw(dev) if raw is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _fits(name: str, t, shape, dtype, dev) -> int:
+    """The tensor's address, if it is a contiguous tensor of this shape and type on this device."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev:
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}: got {t.dtype}, {tuple(t.shape)}, strides {tuple(t.stride())}")
     return t.data_ptr()
 
 
-def _fits_or_none(name: str, t, shape, dtype=None):
-    return None if t is None else _fits(name, t, shape, dtype)
+def _fits_or_none(name: str, t, shape, dtype, dev):
+    return None if t is None else _fits(name, t, shape, dtype, dev)
 
 
-def _room(workspace):
+def _rows_of(name: str, t, dev):
+    """(rows, columns) of a matrix on this device."""
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions: got {tuple(t.shape)}")
+    return t.shape
+
+
+def _current():
+    """_here() where there is a GPU; else a device that no tensor is on, so that the first check refuses."""
+    import torch
+    return _here() if torch.cuda.is_initialized() or torch.cuda.is_available() else (-2, 0)
+
+
+def _room(workspace, dev):
     """(address, bytes) of a workspace, which may be None where none is needed."""
     if workspace is None:
         return None, 0
-    return _fits("workspace", workspace, workspace.shape), _nbytes(workspace)
+    return _fits("workspace", workspace, workspace.shape, workspace.dtype, dev), _nbytes(workspace)
 
 
 def reslim_rmsnorm_fwd(x, gamma, y, *, eps: float = 1e-6, delta=None, sum_out=None, y_scale=None, stream=None) -> None:
@@ -656,11 +678,14 @@ def reslim_rmsnorm_fwd(x, gamma, y, *, eps: float = 1e-6, delta=None, sum_out=No
     activation type; y float8_e4m3fn with y_scale fp32 [rows]; gamma fp32 [D].  Without delta and with an 8-bit y the
     activation type is the stream's."""
     import torch
-    rows, D = x.shape
-    act = delta.dtype if delta is not None else x.dtype if y.dtype == torch.float8_e4m3fn else y.dtype
-    _check(load().reslim_rmsnorm_fwd(_fits("x", x, (rows, D)), _fits_or_none("delta", delta, (rows, D)), _fits("gamma", gamma, (D,), torch.float32),
-                                     eps, rows, D, _code(x.dtype), _code(act), _code(y.dtype), _fits_or_none("sum_out", sum_out, (rows, D), x.dtype),
-                                     _fits("y", y, (rows, D)), _fits_or_none("y_scale", y_scale, (rows,), torch.float32), _stream_ptr(stream)))
+    dev, st = _current()
+    shape = rows, D = _rows_of("x", x, dev)
+    act = delta.dtype if delta is not None else x.dtype if y.dtype is torch.float8_e4m3fn else y.dtype
+    f32 = torch.float32
+    _check(load().reslim_rmsnorm_fwd(_fits("x", x, shape, x.dtype, dev), _fits_or_none("delta", delta, shape, act, dev), _fits("gamma", gamma, (D,), f32, dev),
+                                     eps, rows, D, _code(x.dtype), _code(act), _code(y.dtype), _fits_or_none("sum_out", sum_out, shape, x.dtype, dev),
+                                     _fits("y", y, shape, y.dtype, dev), _fits_or_none("y_scale", y_scale, (rows,), f32, dev),
+                                     st if stream is None else stream.cuda_stream))
 
 
 def reslim_rmsnorm_bwd_workspace_bytes(rows: int, D: int) -> int:
@@ -673,12 +698,14 @@ def reslim_rmsnorm_bwd(sum_in, dy, gamma, dx, dgamma, workspace, *, eps: float =
     """sum_in: the forward's x + delta; d_sum: the gradient that reaches it past the norm (may be dx); dx in the stream's type,
     d_delta the same in dy's; dgamma fp32 [D]."""
     import torch
-    rows, D = sum_in.shape
-    ws, n = _room(workspace)
-    _check(load().reslim_rmsnorm_bwd(_fits("sum_in", sum_in, (rows, D)), _fits("dy", dy, (rows, D)), _fits("gamma", gamma, (D,), torch.float32), eps,
-                                     _fits_or_none("d_sum", d_sum, (rows, D), sum_in.dtype), rows, D, _code(sum_in.dtype), _code(dy.dtype),
-                                     _fits("dx", dx, (rows, D), sum_in.dtype), _fits_or_none("d_delta", d_delta, (rows, D), dy.dtype),
-                                     _fits("dgamma", dgamma, (D,), torch.float32), ws, n, _stream_ptr(stream)))
+    dev, st = _current()
+    shape = rows, D = _rows_of("sum_in", sum_in, dev)
+    f32, s, a = torch.float32, sum_in.dtype, dy.dtype
+    ws, n = _room(workspace, dev)
+    _check(load().reslim_rmsnorm_bwd(_fits("sum_in", sum_in, shape, s, dev), _fits("dy", dy, shape, a, dev), _fits("gamma", gamma, (D,), f32, dev), eps,
+                                     _fits_or_none("d_sum", d_sum, shape, s, dev), rows, D, _code(s), _code(a), _fits("dx", dx, shape, s, dev),
+                                     _fits_or_none("d_delta", d_delta, shape, a, dev), _fits("dgamma", dgamma, (D,), f32, dev), ws, n,
+                                     st if stream is None else stream.cuda_stream))
 
 
 def reslim_rotary_frequencies(rot: int, axes: int = 1, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
@@ -696,19 +723,21 @@ def _rotary(call, x, out, positions, freq, heads, layout, amplitude, stream):
     import torch
     if layout not in ROTARY_LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(ROTARY_LAYOUTS)}")
+    dev, st = _current()
     for name, t in (("x", x), ("out", out)):
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        if t.get_device() != dev:
             raise ValueError(f"{name} is on {t.device}, not on the current GPU")
         if t.dim() != 3 or t.shape[1] < heads or (t.shape[0] > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):
             raise ValueError(f"{name} must be [tokens, at least {heads} heads, dh] with contiguous heads: got {tuple(t.shape)}, strides {tuple(t.stride())}")
     tokens, _, dh = x.shape
-    if out.dtype != x.dtype or out.shape[0] != tokens or out.shape[2] != dh:
+    if out.dtype is not x.dtype or out.shape[0] != tokens or out.shape[2] != dh:
         raise ValueError(f"out must match x in type, tokens and head size: {out.dtype} {tuple(out.shape)} for {x.dtype} {tuple(x.shape)}")
-    axes, period = positions.shape
-    # a dimension of one token may carry any stride
+    axes, period = _rows_of("positions", positions, dev)
+    pairs = freq.numel()
+    # the stride of a dimension of one token says nothing
     xs, os = (t.stride(0) if tokens > 1 else t.shape[1] * dh for t in (x, out))
-    _check(call(x.data_ptr(), out.data_ptr(), _fits("positions", positions, (axes, period), torch.int32), _fits("freq", freq, (freq.numel(),), torch.float64),
-                tokens, xs, os, period, heads, dh, 2 * freq.numel(), axes, ROTARY_LAYOUTS[layout], amplitude, _code(x.dtype), _stream_ptr(stream)))
+    _check(call(x.data_ptr(), out.data_ptr(), _fits("positions", positions, (axes, period), torch.int32, dev), _fits("freq", freq, (pairs,), torch.float64, dev),
+                tokens, xs, os, period, heads, dh, 2 * pairs, axes, ROTARY_LAYOUTS[layout], amplitude, _code(x.dtype), st if stream is None else stream.cuda_stream))
 
 
 def reslim_rotary_fwd(x, out, positions, freq, *, heads: int, layout: str = "half", amplitude: float = 1.0, stream=None) -> None:
@@ -728,14 +757,15 @@ def _gate(gate: str) -> int:
     return GATES[gate]
 
 
-def _gated_weights(w, x, act):
+def _gated_weights(w, x, act, dev):
     """(struct, D, R) of the weights of a gated feed-forward layer: a dict of CUDA tensors w_in [2R, D] in x's type, w_out [D, R] in the
     activations', and where present in_scale, b_in fp32 [2R], b_out fp32 [D]."""
     import torch
-    D, R = w["w_out"].shape
-    return GatedMlpWeightsC(w_in=_fits("w_in", w["w_in"], (2 * R, D), x.dtype), in_scale=_fits_or_none("in_scale", w.get("in_scale"), (2 * R,), torch.float32),
-                            b_in=_fits_or_none("b_in", w.get("b_in"), (2 * R,), torch.float32), w_out=_fits("w_out", w["w_out"], (D, R), act),
-                            b_out=_fits_or_none("b_out", w.get("b_out"), (D,), torch.float32)), D, R
+    f32 = torch.float32
+    D, R = _rows_of("w_out", w["w_out"], dev)
+    return GatedMlpWeightsC(_fits("w_in", w["w_in"], (2 * R, D), x.dtype, dev), _fits_or_none("in_scale", w.get("in_scale"), (2 * R,), f32, dev),
+                            _fits_or_none("b_in", w.get("b_in"), (2 * R,), f32, dev), _fits("w_out", w["w_out"], (D, R), act, dev),
+                            _fits_or_none("b_out", w.get("b_out"), (D,), f32, dev)), D, R
 
 
 def reslim_gated_mlp_workspace_bytes(rows: int, D: int, R: int, dtype) -> int:
@@ -748,22 +778,25 @@ def reslim_gated_mlp_workspace_bytes(rows: int, D: int, R: int, dtype) -> int:
 def reslim_gated_mlp_fwd(x, weights, y, workspace, *, gate: str = "silu", x_scale=None, stream=None) -> None:
     """y = (act(x Wg^T + bg) * (x Wu^T + bu)) Wo^T + bo; x [rows, D] fp32, bf16, or float8_e4m3fn with x_scale fp32 [rows]."""
     import torch
-    act = torch.bfloat16 if x.dtype == torch.float8_e4m3fn else x.dtype
-    w, D, R = _gated_weights(weights, x, act)
-    rows = x.shape[0]
-    ws, n = _room(workspace)
-    _check(load().reslim_gated_mlp_fwd(_fits("x", x, (rows, D)), _fits_or_none("x_scale", x_scale, (rows,), torch.float32), C.byref(w), _gate(gate),
-                                       rows, D, R, _code(x.dtype), _fits("y", y, (rows, D), act), ws, n, _stream_ptr(stream)))
+    dev, st = _current()
+    act = torch.bfloat16 if x.dtype is torch.float8_e4m3fn else x.dtype
+    rows = _rows_of("x", x, dev)[0]
+    w, D, R = _gated_weights(weights, x, act, dev)
+    ws, n = _room(workspace, dev)
+    _check(load().reslim_gated_mlp_fwd(_fits("x", x, (rows, D), x.dtype, dev), _fits_or_none("x_scale", x_scale, (rows,), torch.float32, dev), C.byref(w),
+                                       _gate(gate), rows, D, R, _code(x.dtype), _fits("y", y, (rows, D), act, dev), ws, n,
+                                       st if stream is None else stream.cuda_stream))
 
 
 def reslim_gated_mlp_fwd_train(x, weights, gu, h, y, workspace, *, gate: str = "silu", stream=None) -> None:
     """reslim_gated_mlp_fwd that also writes gu [rows, 2R] and h [rows, R], which reslim_gated_mlp_bwd reads."""
-    w, D, R = _gated_weights(weights, x, x.dtype)
-    rows = x.shape[0]
-    ws, n = _room(workspace)
-    _check(load().reslim_gated_mlp_fwd_train(_fits("x", x, (rows, D)), C.byref(w), _gate(gate), rows, D, R, _code(x.dtype),
-                                             _fits("gu", gu, (rows, 2 * R), x.dtype), _fits("h", h, (rows, R), x.dtype), _fits("y", y, (rows, D), x.dtype),
-                                             ws, n, _stream_ptr(stream)))
+    dev, st = _current()
+    t = x.dtype
+    rows = _rows_of("x", x, dev)[0]
+    w, D, R = _gated_weights(weights, x, t, dev)
+    ws, n = _room(workspace, dev)
+    _check(load().reslim_gated_mlp_fwd_train(_fits("x", x, (rows, D), t, dev), C.byref(w), _gate(gate), rows, D, R, _code(t), _fits("gu", gu, (rows, 2 * R), t, dev),
+                                             _fits("h", h, (rows, R), t, dev), _fits("y", y, (rows, D), t, dev), ws, n, st if stream is None else stream.cuda_stream))
 
 
 def reslim_gated_mlp_bwd_workspace_bytes(rows: int, D: int, R: int, dtype, grad_dtype) -> int:
@@ -774,14 +807,16 @@ def reslim_gated_mlp_bwd_workspace_bytes(rows: int, D: int, R: int, dtype, grad_
 
 def reslim_gated_mlp_bwd(x, gu, h, dy, weights, dx, grads, workspace, *, gate: str = "silu", stream=None) -> None:
     """grads: dict of CUDA tensors w_in, w_out and, where wanted, b_in, b_out, all fp32 or all bf16 (written); dx [rows, D] or None."""
-    w, D, R = _gated_weights(weights, x, x.dtype)
-    rows, gt = x.shape[0], grads["w_in"].dtype
-    g = GatedMlpGradsC(w_in=_fits("grads w_in", grads["w_in"], (2 * R, D), gt), b_in=_fits_or_none("grads b_in", grads.get("b_in"), (2 * R,), gt),
-                       w_out=_fits("grads w_out", grads["w_out"], (D, R), gt), b_out=_fits_or_none("grads b_out", grads.get("b_out"), (D,), gt))
-    ws, n = _room(workspace)
-    _check(load().reslim_gated_mlp_bwd(_fits("x", x, (rows, D)), _fits("gu", gu, (rows, 2 * R), x.dtype), _fits("h", h, (rows, R), x.dtype),
-                                       _fits("dy", dy, (rows, D), x.dtype), C.byref(w), _gate(gate), rows, D, R, _code(x.dtype), _code(gt),
-                                       _fits_or_none("dx", dx, (rows, D), x.dtype), C.byref(g), ws, n, _stream_ptr(stream)))
+    dev, st = _current()
+    t, gt = x.dtype, grads["w_in"].dtype
+    rows = _rows_of("x", x, dev)[0]
+    w, D, R = _gated_weights(weights, x, t, dev)
+    g = GatedMlpGradsC(_fits("grads w_in", grads["w_in"], (2 * R, D), gt, dev), _fits_or_none("grads b_in", grads.get("b_in"), (2 * R,), gt, dev),
+                       _fits("grads w_out", grads["w_out"], (D, R), gt, dev), _fits_or_none("grads b_out", grads.get("b_out"), (D,), gt, dev))
+    ws, n = _room(workspace, dev)
+    _check(load().reslim_gated_mlp_bwd(_fits("x", x, (rows, D), t, dev), _fits("gu", gu, (rows, 2 * R), t, dev), _fits("h", h, (rows, R), t, dev),
+                                       _fits("dy", dy, (rows, D), t, dev), C.byref(w), _gate(gate), rows, D, R, _code(t), _code(gt),
+                                       _fits_or_none("dx", dx, (rows, D), t, dev), C.byref(g), ws, n, st if stream is None else stream.cuda_stream))
 
 
 # ------------------------------------------------------------------ convenience holder

@@ -62,16 +62,24 @@ struct GatedIn {                       // x W_in^T and what follows up to the hi
 };
 hipError_t gated_gemm_init();
 hipError_t launch_gated_in(const GatedIn &g, bool gelu, hipStream_t st);
+// the same for few rows, any type (gated_token.hip); rows of x, W_in, h and W_out are multiples of 64 bytes
+hipError_t launch_gated_token_in(int x_dtype, const GatedIn &g, bool gelu, hipStream_t st);
+hipError_t launch_gated_token_out(int dtype, const void *h, const void *w_out, const float *b_out, void *y, int M, int D, int R, hipStream_t st);
+// out [M, N] bf16 = a [M, K] w [N, K]^T (+ bias, may be null), the sum over k cut into slices where one tile a work-group would leave compute units
+// idle; part: gated_slices() M N floats
+int gated_slices(int M, int N, int K);
+hipError_t launch_gated_sliced(const void *a, const void *w, const float *bias, void *out, int M, int N, int K, float *part, hipStream_t st);
 // d_gu [M, 2R] from dy [M, D], the transposed output map wt_out [R, D] and the forward's gu
 hipError_t launch_gated_dgate(const void *dy, const void *wt_out, const void *gu, void *d_gu, int M, int D, int R, bool gelu, hipStream_t st);
 // dst [C, R] (rows ld apart) = src [R, C]^T, bf16, both matrices of the layer in one launch
 hipError_t launch_gated_transpose(const void *w_in, void *wt_in, const void *w_out, void *wt_out, int D, int R, hipStream_t st);
 
-// fp32: C[M, N] = A B^T + bias with any strides; see gated_f32.hip
+// fp32, any sizes; see gated_f32.hip.  part: partial sums of the slices of a product [M, N] over K, gated_f32_product_bytes()
+size_t gated_f32_product_bytes(int M, int N, int K);
 hipError_t launch_gated_f32_in(const GatedIn &g, bool gelu, hipStream_t st);
-hipError_t launch_gated_f32_out(const float *h, const float *w_out, const float *b_out, float *y, int M, int D, int R, hipStream_t st);
+hipError_t launch_gated_f32_out(const float *h, const float *w_out, const float *b_out, float *y, int M, int D, int R, float *part, hipStream_t st);
 hipError_t launch_gated_f32_dgate(const float *dy, const float *w_out, const float *gu, float *d_gu, int M, int D, int R, bool gelu, hipStream_t st);
-hipError_t launch_gated_f32_dx(const float *d_gu, const float *w_in, float *dx, int M, int D, int R, hipStream_t st);
+hipError_t launch_gated_f32_dx(const float *d_gu, const float *w_in, float *dx, int M, int D, int R, float *part, hipStream_t st);
 // dw [N, K] = dy[M, N]^T x[M, K], db (or null) = column sums of dy
 size_t gated_f32_wgrad_bytes(int M, int N, int K);
 hipError_t launch_gated_f32_wgrad(const float *dy, const float *x, float *dw, float *db, int M, int N, int K, void *ws, hipStream_t st);

@@ -48,9 +48,18 @@ __global__ __launch_bounds__(256) void gated_zero_kernel(ZeroArgs a) {
 }
 
 // ------------------------------------------------------------------ workspaces
+static size_t gated_hidden_bytes(int M, int R, int x_dtype) { return align256(static_cast<size_t>(M) * R * (x_dtype == RESLIM_F32 ? 4 : 2)); }
+// partial sums of a product's slices: out [M, N] over K
+static size_t gated_part_bytes(int M, int N, int K, int x_dtype) {
+  if (M < 1) return 0;
+  if (x_dtype == RESLIM_F32) return gated_f32_product_bytes(M, N, K);
+  const int s = gated_slices(M, N, K);
+  return s > 1 ? align256(static_cast<size_t>(s) * M * N * sizeof(float)) : 0;
+}
 struct GatedBwdWs {
   void *d_gu;                  // act [M, 2R]
   void *wt_in, *wt_out;        // bf16 [D, 2R], [R, D]
+  void *part;                  // partial sums of dx
   void *wgrad;                 // partial sums of the parameter gradients
   void *sink_in, *sink_out;    // 2R and D floats: bias gradients that nobody asked for
   size_t total;
@@ -66,6 +75,7 @@ static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, int grad_dtype,
   const size_t es = type_bytes(dtype), m = M, d = D, r = R;
   GatedBwdWs w = {};
   w.d_gu = take(m * 2 * r * es);
+  w.part = take(gated_part_bytes(M, D, 2 * R, dtype));
   if (dtype == RESLIM_BF16) {
     w.wt_in = take(2 * r * d * 2);
     w.wt_out = take(r * d * 2);
@@ -80,13 +90,13 @@ static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, int grad_dtype,
   w.total = off;
   return w;
 }
-static size_t gated_fwd_bytes(int M, int R, int x_dtype) { return align256(static_cast<size_t>(M) * R * (x_dtype == RESLIM_F32 ? 4 : 2)); }
+static size_t gated_fwd_bytes(int M, int D, int R, int x_dtype) { return gated_part_bytes(M, D, R, x_dtype) + gated_hidden_bytes(M, R, x_dtype); }
 
 // ------------------------------------------------------------------ checks
 static int gated_shape(const char *fn, int rows, int D, int R, int x_dtype) {
   if (x_dtype != RESLIM_F32 && x_dtype != RESLIM_BF16 && x_dtype != RESLIM_E4M3) return refuse(RESLIM_EINVAL, fn, "x_dtype must be RESLIM_F32, RESLIM_BF16 or RESLIM_E4M3");
   if (rows < 0 || D < 1 || D > kGatedMaxD || R < 1 || R > kGatedMaxR) return refuse(RESLIM_ESHAPE, fn, "need rows >= 0, 1 <= D <= 16384 and 1 <= R <= 65536");
-  if (x_dtype == RESLIM_F32 && rows > 8000000) return refuse(RESLIM_ESHAPE, fn, "the fp32 path takes up to 8,000,000 rows");
+  if (x_dtype == RESLIM_F32 && rows > 4000000) return refuse(RESLIM_ESHAPE, fn, "the fp32 path takes up to 4,000,000 rows");
   if (x_dtype == RESLIM_BF16 && (D % 64 || R % 64)) return refuse(RESLIM_ESHAPE, fn, "bf16 needs D and R to be multiples of 64");
   if (x_dtype == RESLIM_E4M3 && (D % 128 || R % 64)) return refuse(RESLIM_ESHAPE, fn, "e4m3 needs D to be a multiple of 128 and R of 64");
   return RESLIM_OK;
@@ -112,10 +122,26 @@ static int gated_room(const char *fn, const void *ws, size_t ws_bytes, size_t ne
   return refuse(RESLIM_EWORKSPACE, fn, "workspace null, not 256-byte aligned or smaller than the workspace query says");
 }
 
-static hipError_t gated_forward(const GatedIn &in, const reslim_gated_mlp_weights *w, bool f32, bool gelu, void *y, const float *zeros, hipStream_t st) {
-  hipError_t e = f32 ? launch_gated_f32_in(in, gelu, st) : launch_gated_in(in, gelu, st);
+// Few rows: the weights' bytes bound both products, and streaming them past the token rows beats tiles, bf16 at 4096 x 10,944 (both products, us):
+// 1 row 67 against 171 (79 with the output map in slices), 8 rows 76 against 79, 16 rows 89 against 81.  The fp32 tiles have no persistent kernel
+// behind them: up to 64 rows.
+static bool gated_few(int x_dtype, int M, int D, int R, const GatedIn &in, const reslim_gated_mlp_weights *w) {
+  const int es = x_dtype == RESLIM_F32 ? 4 : 2;
+  if (M > (x_dtype == RESLIM_F32 ? 64 : 8) || D * type_bytes(x_dtype) % 64 || R * es % 64) return false;
+  return x_dtype != RESLIM_F32 || (aligned(in.x, 16) && aligned(in.w_in, 16) && aligned(in.h, 16) && aligned(w->w_out, 16));
+}
+
+static hipError_t gated_forward(const GatedIn &in, const reslim_gated_mlp_weights *w, int x_dtype, bool gelu, void *y, void *part, const float *zeros, hipStream_t st) {
+  const int dtype = x_dtype == RESLIM_F32 ? RESLIM_F32 : RESLIM_BF16;
+  if (gated_few(x_dtype, in.M, in.D, in.R, in, w)) {
+    const hipError_t e = launch_gated_token_in(x_dtype, in, gelu, st);
+    return e == hipSuccess ? launch_gated_token_out(dtype, in.h, w->w_out, w->b_out, y, in.M, in.D, in.R, st) : e;
+  }
+  const bool f32 = x_dtype == RESLIM_F32;
+  const hipError_t e = f32 ? launch_gated_f32_in(in, gelu, st) : launch_gated_in(in, gelu, st);
   if (e != hipSuccess) return e;
-  if (f32) return launch_gated_f32_out(static_cast<const float *>(in.h), static_cast<const float *>(w->w_out), w->b_out, static_cast<float *>(y), in.M, in.D, in.R, st);
+  if (f32) return launch_gated_f32_out(static_cast<const float *>(in.h), static_cast<const float *>(w->w_out), w->b_out, static_cast<float *>(y), in.M, in.D, in.R, static_cast<float *>(part), st);
+  if (gated_slices(in.M, in.D, in.R) > 1) return launch_gated_sliced(in.h, w->w_out, w->b_out, y, in.M, in.D, in.R, static_cast<float *>(part), st);
   return launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, in.h, w->w_out, w->b_out ? w->b_out : zeros, y, in.D, nullptr, 0, in.M, in.D, in.R, st);
 }
 
@@ -127,8 +153,11 @@ extern "C" int reslim_gated_mlp_workspace_bytes(int32_t rows, int32_t D, int32_t
   const char *fn = "reslim_gated_mlp_workspace_bytes";
   if (!out) return refuse(RESLIM_EINVAL, fn, "null argument");
   const int rc = gated_shape(fn, rows, D, R, x_dtype);
-  if (rc == RESLIM_OK) *out = gated_fwd_bytes(rows, R, x_dtype);
-  return rc;
+  if (rc != RESLIM_OK) return rc;
+  const float *zeros = nullptr;
+  if (x_dtype != RESLIM_F32) (void)gated_ready(&zeros);      // the slices go by the device's compute units
+  *out = gated_fwd_bytes(rows, D, R, x_dtype);
+  return RESLIM_OK;
 }
 
 extern "C" int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const reslim_gated_mlp_weights *w, int32_t gate, int32_t rows, int32_t D, int32_t R,
@@ -138,12 +167,13 @@ extern "C" int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const r
   if (rc != RESLIM_OK) return rc;
   if (rows > 0 && (x_dtype == RESLIM_E4M3) != (x_scale != nullptr)) return refuse(RESLIM_EINVAL, fn, "x_scale goes with RESLIM_E4M3, and only with it");
   if (!aligned(x_scale, 4)) return refuse(RESLIM_EINVAL, fn, "a buffer is not aligned to its elements");
-  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, R, x_dtype))) != RESLIM_OK) return rc;
+  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, D, R, x_dtype))) != RESLIM_OK) return rc;
   if (rows == 0) return RESLIM_OK;
   const float *zeros = nullptr;
   hipError_t e = gated_ready(&zeros);
-  const GatedIn in = {x, w->w_in, x_scale, w->in_scale, w->b_in, nullptr, workspace, rows, D, R};
-  if (e == hipSuccess) e = gated_forward(in, w, x_dtype == RESLIM_F32, gate == RESLIM_GATE_GELU, y, zeros, static_cast<hipStream_t>(hip_stream));
+  unsigned char *h = static_cast<unsigned char *>(workspace) + gated_part_bytes(rows, D, R, x_dtype);
+  const GatedIn in = {x, w->w_in, x_scale, w->in_scale, w->b_in, nullptr, h, rows, D, R};
+  if (e == hipSuccess) e = gated_forward(in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
 }
 
@@ -153,12 +183,12 @@ extern "C" int reslim_gated_mlp_fwd_train(const void *x, const reslim_gated_mlp_
   int rc = gated_check(fn, w, gate, rows, D, R, x_dtype, {x, gu, h, y}, {});
   if (rc != RESLIM_OK) return rc;
   if (x_dtype == RESLIM_E4M3) return refuse(RESLIM_EINVAL, fn, "training takes RESLIM_F32 or RESLIM_BF16");
-  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, R, x_dtype))) != RESLIM_OK) return rc;
+  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, D, R, x_dtype))) != RESLIM_OK) return rc;
   if (rows == 0) return RESLIM_OK;
   const float *zeros = nullptr;
   hipError_t e = gated_ready(&zeros);
   const GatedIn in = {x, w->w_in, nullptr, nullptr, w->b_in, gu, h, rows, D, R};
-  if (e == hipSuccess) e = gated_forward(in, w, x_dtype == RESLIM_F32, gate == RESLIM_GATE_GELU, y, zeros, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = gated_forward(in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
 }
 
@@ -207,14 +237,16 @@ extern "C" int reslim_gated_mlp_bwd(const void *x, const void *gu, const void *h
     auto f = [](const void *p) { return static_cast<const float *>(p); };
     auto o = [](void *p) { return static_cast<float *>(p); };
     e = launch_gated_f32_dgate(f(dy), f(w->w_out), f(gu), o(ws.d_gu), rows, D, R, gelu, st);
-    if (e == hipSuccess && dx) e = launch_gated_f32_dx(f(ws.d_gu), f(w->w_in), o(dx), rows, D, R, st);
+    if (e == hipSuccess && dx) e = launch_gated_f32_dx(f(ws.d_gu), f(w->w_in), o(dx), rows, D, R, o(ws.part), st);
     if (e == hipSuccess) e = launch_gated_f32_wgrad(f(ws.d_gu), f(x), o(grads->w_in), o(grads->b_in), rows, 2 * R, D, ws.wgrad, st);
     if (e == hipSuccess) e = launch_gated_f32_wgrad(f(dy), f(h), o(grads->w_out), o(grads->b_out), rows, D, R, ws.wgrad, st);
     return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
   }
   e = launch_gated_transpose(w->w_in, ws.wt_in, w->w_out, ws.wt_out, D, R, st);
   if (e == hipSuccess) e = launch_gated_dgate(dy, ws.wt_out, gu, ws.d_gu, rows, D, R, gelu, st);
-  if (e == hipSuccess && dx) e = launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, ws.d_gu, ws.wt_in, zeros, dx, D, nullptr, 0, rows, D, 2 * R, st);
+  if (e == hipSuccess && dx)
+    e = gated_slices(rows, D, 2 * R) > 1 ? launch_gated_sliced(ws.d_gu, ws.wt_in, nullptr, dx, rows, D, 2 * R, static_cast<float *>(ws.part), st)
+                                         : launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, ws.d_gu, ws.wt_in, zeros, dx, D, nullptr, 0, rows, D, 2 * R, st);
   if (e == hipSuccess) {
     WgradOp op[2];
     gated_ops(op, ws.d_gu, x, dy, h, D, R);

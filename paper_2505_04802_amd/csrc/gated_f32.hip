@@ -1,9 +1,10 @@
 // The gated feed-forward layer's products on the fp32 path, for small problems and parity: any sizes, any operand order.
 //
-//   C[m, n] = sum_k A(m, k) B(n, k), fp32 matrix instructions (v_mfma_f32_32x32x2), tiles of 128 x 64, slabs of 16 k staged through
-// LDS as [row][k] whichever way the operands lie in memory, so that one kernel serves the forward products, the gradients of
-// their inputs (B read across its rows) and of the weights (both read across, the sum over the tokens cut into slices that are
-// added in order where there are few tiles).  A gated tile is 32 gate and 32 up rows of the same features.
+//   C[m, n] = sum_k A(m, k) B(n, k), fp32 matrix instructions (v_mfma_f32_32x32x2), tiles of 64 x 64 with a 32 x 32 block for each of
+// four waves, slabs of 32 k in two LDS buffers, the next slab's loads in flight in registers.  An operand whose k is contiguous is staged as
+// [row][k], one whose rows are as [k][row], both with 16-byte loads, so that one kernel serves the forward products, the gradients of their inputs (B
+// read across its rows) and of the weights (both read across).  Where there are few tiles, k is cut into slices that are added in
+// order.  A gated block is 16 gate and 16 up rows of the same features; lanes 16 apart exchange them.
 #include <algorithm>
 #include <type_traits>
 
@@ -24,118 +25,126 @@ struct F32Args {
   int64_t slice;                       // floats between the slices' results
 };
 
-constexpr int kBM = 128, kBN = 64, kBK = 16, kPitch = 20;      // rows of 20 floats: the 16-byte reads of 8 rows fall into different banks
+constexpr int kTile = 64, kBK = 32;
+constexpr int kPitchK = 36, kPitchRow = 68;      // floats of a [row][k] row and of a [k][row] one: 16-byte accesses of neighbouring rows fall into different banks
 
-// one operand's slab: ROWS x 16 values, `row0` its first row of `rows`, `k0` .. `k_end`; a thread holds ROWS / 16 of them
-template <int ROWS, bool ALONG_K>
+// one operand's slab of 64 x 32 values from row `row0`, k `k0` on, eight of them a thread.  row_of: the operand's row for a row of the tile, or -1
+template <bool ALONG_K>
 struct Slab {
-  static constexpr int kEach = ROWS / 16;
-  float v[kEach];
+  static constexpr int kFloats = ALONG_K ? kTile * kPitchK : kBK * kPitchRow;
+  float v[8];
   template <class RowOf>
   __device__ __forceinline__ void load(const float *p, int64_t step, bool vec, int k0, int k_end, RowOf &&row_of) {
     const int t = threadIdx.x;
-    if constexpr (ALONG_K) {                 // 16 / kEach threads to a row, each kEach consecutive k
-      constexpr int PER = kBK / kEach;
-      const int row = row_of(t / PER), k = k0 + t % PER * kEach;
-      const float *q = p + static_cast<int64_t>(row) * step + k;
-      if (vec && row >= 0 && k + kEach <= k_end) {
-#pragma unroll
-        for (int i = 0; i < kEach; i += 4) {
-          const float4 f = *reinterpret_cast<const float4 *>(q + i);
-          v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
-        }
+    if constexpr (ALONG_K) {                 // four threads to a row, eight consecutive k each
+      const int row = row_of(t / 4), k = k0 + t % 4 * 8;
+      const float *q = p + static_cast<int64_t>(row < 0 ? 0 : row) * step;
+      if (vec && row >= 0 && k + 8 <= k_end) {
+        fetch8(q + k);
       } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = row >= 0 && k + i < k_end ? q[i] : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = row >= 0 && k + i < k_end ? q[k + i] : 0.f;
       }
-    } else {                                 // sixteen threads to a k, each kEach consecutive rows
-      const int k = k0 + t / 16, first = t % 16 * kEach;
-      const bool in = k < k_end;
-      const int r0 = row_of(first), r1 = row_of(first + kEach - 1);
-      const float *q = p + static_cast<int64_t>(in ? k : 0) * step;
-      if (vec && in && r0 >= 0 && r1 == r0 + kEach - 1) {
-#pragma unroll
-        for (int i = 0; i < kEach; i += 4) {
-          const float4 f = *reinterpret_cast<const float4 *>(q + r0 + i);
-          v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
-        }
+    } else {                                 // eight threads to a k, eight consecutive rows each
+      const int k = k0 + t / 8, first = t % 8 * 8;
+      const int r0 = row_of(first), r1 = row_of(first + 7);
+      const float *q = p + static_cast<int64_t>(k < k_end ? k : k0) * step;
+      if (vec && k < k_end && r0 >= 0 && r1 == r0 + 7) {
+        fetch8(q + r0);
       } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
+        for (int i = 0; i < 8; ++i) {
           const int r = row_of(first + i);
-          v[i] = in && r >= 0 ? q[r] : 0.f;
+          v[i] = k < k_end && r >= 0 ? q[r] : 0.f;
         }
       }
     }
   }
+  __device__ __forceinline__ void fetch8(const float *q) {
+    const float4 a = *reinterpret_cast<const float4 *>(q), b = *reinterpret_cast<const float4 *>(q + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
   __device__ __forceinline__ void store(float *lds) const {
     const int t = threadIdx.x;
+    float *q = lds + (ALONG_K ? t / 4 * kPitchK + t % 4 * 8 : t / 8 * kPitchRow + t % 8 * 8);
+    *reinterpret_cast<float4 *>(q) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4 *>(q + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  // four consecutive k of a row of the tile
+  static __device__ __forceinline__ void read(const float *lds, int row, int k, float (&f)[4]) {
     if constexpr (ALONG_K) {
-      constexpr int PER = kBK / kEach;
-      float *q = lds + t / PER * kPitch + t % PER * kEach;
-#pragma unroll
-      for (int i = 0; i < kEach; i += 4) *reinterpret_cast<float4 *>(q + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      const float4 x = *reinterpret_cast<const float4 *>(lds + row * kPitchK + k);
+      f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
     } else {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) lds[(t % 16 * kEach + i) * kPitch + t / 16] = v[i];
+      for (int i = 0; i < 4; ++i) f[i] = lds[(k + i) * kPitchRow + row];
     }
   }
 };
 
 template <F32Kind KIND, bool GELU, bool A_ALONG, bool B_ALONG>
 __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
-  __shared__ __align__(16) float As[kBM * kPitch], Bs[kBN * kPitch];
-  constexpr int BNO = KIND == kGate ? kBN / 2 : kBN;
+  __shared__ __align__(16) float As[2][Slab<A_ALONG>::kFloats], Bs[2][Slab<B_ALONG>::kFloats];
+  constexpr int BNO = KIND == kGate ? kTile / 2 : kTile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l32 = lane & 31, hi = lane >> 5;
-  const int n0 = blockIdx.x * BNO, m0 = blockIdx.y * kBM;
+  const int l32 = lane & 31, hi = lane >> 5, wm = wave >> 1, wn = wave & 1;
+  const int n0 = blockIdx.x * BNO, m0 = blockIdx.y * kTile;
   const int k_begin = blockIdx.z * g.k_per, k_end = min(g.K, k_begin + g.k_per);
   auto a_row = [&](int r) { return m0 + r < g.M ? m0 + r : -1; };
   auto b_row = [&](int r) {
-    if constexpr (KIND == kGate) return n0 + (r & 31) < g.N ? n0 + (r & 31) + (r & 32 ? g.N : 0) : -1;
-    else return n0 + r < g.N ? n0 + r : -1;
+    if constexpr (KIND == kGate) {
+      const int n = n0 + (r >> 5) * 16 + (r & 15);
+      return n < g.N ? n + (r & 16 ? g.N : 0) : -1;
+    } else {
+      return n0 + r < g.N ? n0 + r : -1;
+    }
   };
+  static_assert(KIND != kGate || B_ALONG, "a gated tile's rows are not in a run");
   const bool a_vec = g.a_step % 4 == 0 && (reinterpret_cast<uintptr_t>(g.a) & 15) == 0;
-  // rows of a gated tile's halves start anywhere when N is no multiple of four
-  const bool b_vec = g.b_step % 4 == 0 && (reinterpret_cast<uintptr_t>(g.b) & 15) == 0 && (B_ALONG || KIND != kGate || g.N % 4 == 0);
-  Slab<kBM, A_ALONG> sa;
-  Slab<kBN, B_ALONG> sb;
-  f32x16 acc[2] = {};
+  const bool b_vec = g.b_step % 4 == 0 && (reinterpret_cast<uintptr_t>(g.b) & 15) == 0;
+  Slab<A_ALONG> sa;
+  Slab<B_ALONG> sb;
+  f32x16 acc = {};
   sa.load(g.a, g.a_step, a_vec, k_begin, k_end, a_row);
   sb.load(g.b, g.b_step, b_vec, k_begin, k_end, b_row);
-  for (int k0 = k_begin; k0 < k_end; k0 += kBK) {
-    __syncthreads();
-    sa.store(As);
-    sb.store(Bs);
-    __syncthreads();
-    if (k0 + kBK < k_end) {
+  sa.store(As[0]);
+  sb.store(Bs[0]);
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += kBK, buf ^= 1) {
+    const bool more = k0 + kBK < k_end;
+    if (more) {
       sa.load(g.a, g.a_step, a_vec, k0 + kBK, k_end, a_row);
       sb.load(g.b, g.b_step, b_vec, k0 + kBK, k_end, b_row);
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float4 x = *reinterpret_cast<const float4 *>(&As[(wave * 32 + l32) * kPitch + 8 * s + 4 * hi]);
-      float4 w[2];
+    for (int s = 0; s < kBK / 8; ++s) {
+      float x[4], w[4];
+      Slab<A_ALONG>::read(As[buf], wm * 32 + l32, 8 * s + 4 * hi, x);
+      Slab<B_ALONG>::read(Bs[buf], wn * 32 + l32, 8 * s + 4 * hi, w);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) w[j] = *reinterpret_cast<const float4 *>(&Bs[(j * 32 + l32) * kPitch + 8 * s + 4 * hi]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {          // operands swapped: the block is C^T
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j].x, x.x, acc[j], 0, 0, 0);
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j].y, x.y, acc[j], 0, 0, 0);
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j].z, x.z, acc[j], 0, 0, 0);
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j].w, x.w, acc[j], 0, 0, 0);
-      }
+      for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], w[i], acc, 0, 0, 0);
     }
+    if (more) {                              // the other buffer was last read before the barrier that ended the slab before
+      sa.store(As[buf ^ 1]);
+      sb.store(Bs[buf ^ 1]);
+    }
+    __syncthreads();
   }
-  // register r of a block: row l32, column 8 (r / 4) + 4 hi + r % 4
-  const int m = m0 + wave * 32 + l32;
-  if (m >= g.M) return;
+  // register r of the block: row 8 (r / 4) + 4 hi + r % 4, column l32: a store writes runs of 32 columns of two rows
+  const int row0 = m0 + wm * 32 + 4 * hi;
+  auto row_of = [&](int r) { return row0 + 8 * (r / 4) + r % 4; };
   if constexpr (KIND == kGate) {
+    // columns 0 .. 15 of the block are gates, 16 .. 31 the same features' up projections: the lanes of either half get the other value of eight rows
+    const bool up_lane = l32 & 16;
+    const int n = n0 + wn * 16 + (l32 & 15);
+    const float bg = g.bias && n < g.N ? g.bias[n] : 0.f, bu = g.bias && n < g.N ? g.bias[g.N + n] : 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int n = n0 + 8 * (r / 4) + 4 * hi + r % 4;
-      if (n >= g.N) continue;
-      const float gate = acc[0][r] + (g.bias ? g.bias[n] : 0.f), up = acc[1][r] + (g.bias ? g.bias[g.N + n] : 0.f);
+    for (int r = 0; r < 8; ++r) {
+      const float mine = up_lane ? acc[r + 8] : acc[r], other = __shfl_xor(up_lane ? acc[r] : acc[r + 8], 16);
+      const float gate = (up_lane ? other : mine) + bg, up = (up_lane ? mine : other) + bu;
+      const int m = row_of(up_lane ? r + 8 : r);
+      if (m >= g.M || n >= g.N) continue;
       if (g.keep) {
         g.keep[static_cast<int64_t>(m) * 2 * g.N + n] = gate;
         g.keep[static_cast<int64_t>(m) * 2 * g.N + g.N + n] = up;
@@ -143,45 +152,48 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
       g.out[static_cast<int64_t>(m) * g.N + n] = gate_act_f32<GELU>(gate) * up;
     }
   } else {
+    const int n = n0 + wn * 32 + l32;
+    if (n >= g.N) return;
+    const float bias = g.bias && blockIdx.z == 0 ? g.bias[n] : 0.f;      // the first slice brings the bias
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = n0 + j * 32 + 8 * (r / 4) + 4 * hi + r % 4;
-        if (n >= g.N) continue;
-        if constexpr (KIND == kDGate) {
-          const int64_t at = static_cast<int64_t>(m) * 2 * g.N + n;
-          float act, slope;
-          gate_act_slope_f32<GELU>(g.gu[at], act, slope);
-          g.out[at] = acc[j][r] * g.gu[at + g.N] * slope;
-          g.out[at + g.N] = acc[j][r] * act;
-        } else {
-          g.out[blockIdx.z * g.slice + static_cast<int64_t>(m) * g.N + n] = acc[j][r] + (g.bias ? g.bias[n] : 0.f);
-        }
+    for (int r = 0; r < 16; ++r) {
+      const int m = row_of(r);
+      if (m >= g.M) continue;
+      if constexpr (KIND == kDGate) {
+        const int64_t at = static_cast<int64_t>(m) * 2 * g.N + n;
+        float act, slope;
+        gate_act_slope_f32<GELU>(g.gu[at], act, slope);
+        g.out[at] = acc[r] * g.gu[at + g.N] * slope;
+        g.out[at + g.N] = acc[r] * act;
+      } else {
+        g.out[blockIdx.z * g.slice + static_cast<int64_t>(m) * g.N + n] = acc[r] + bias;
       }
+    }
   }
 }
 
 // column sums of a [rows, N] matrix, a slab of rows for each work-group of 64 columns: partial [slabs, N]
-constexpr int kSumRows = 256;
+constexpr int kSumRows = 64;
 __global__ __launch_bounds__(256) void gated_colsum_kernel(const float *__restrict__ a, float *__restrict__ partial, int64_t rows, int N) {
   __shared__ float sm[4][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), grp = threadIdx.x >> 6;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kSumRows, r1 = min(rows, r0 + kSumRows);
   float s = 0.f;
-  if (c < N)
+  if (c < N) {
+#pragma unroll 8
     for (int64_t r = r0 + grp; r < r1; r += 4) s += a[r * N + c];
+  }
   sm[grp][threadIdx.x & 63] = s;
   __syncthreads();
   if (grp == 0 && c < N) partial[static_cast<int64_t>(blockIdx.y) * N + c] = (sm[0][threadIdx.x] + sm[1][threadIdx.x]) + (sm[2][threadIdx.x] + sm[3][threadIdx.x]);
 }
 
 template <F32Kind KIND, bool GELU, bool A_ALONG, bool B_ALONG>
-hipError_t launch(F32Args g, int splits, hipStream_t st) {
-  constexpr int BNO = KIND == kGate ? kBN / 2 : kBN;
-  const int64_t gm = (static_cast<int64_t>(g.M) + kBM - 1) / kBM;
-  if (gm > 65535 || splits > 65535) return hipErrorInvalidValue;
-  gated_f32_kernel<KIND, GELU, A_ALONG, B_ALONG><<<dim3((g.N + BNO - 1) / BNO, static_cast<unsigned>(gm), splits), dim3(256), 0, st>>>(g);
+hipError_t launch(const F32Args &g, int slices, hipStream_t st) {
+  constexpr int BNO = KIND == kGate ? kTile / 2 : kTile;
+  const int64_t gm = (static_cast<int64_t>(g.M) + kTile - 1) / kTile;
+  if (gm > 65535 || slices > 65535) return hipErrorInvalidValue;
+  gated_f32_kernel<KIND, GELU, A_ALONG, B_ALONG><<<dim3((g.N + BNO - 1) / BNO, static_cast<unsigned>(gm), slices), dim3(256), 0, st>>>(g);
   return hipGetLastError();
 }
 F32Args whole(const float *a, int64_t a_step, const float *b, int64_t b_step, float *out, int M, int N, int K) {
@@ -191,10 +203,28 @@ F32Args whole(const float *a, int64_t a_step, const float *b, int64_t b_step, fl
   return g;
 }
 
-// Slices of the tokens: as many as give every compute unit two tiles, of at least 256 tokens each.
-int wgrad_slices(int M, int N, int K) {
-  const int64_t tiles = (static_cast<int64_t>(N) + kBM - 1) / kBM * ((static_cast<int64_t>(K) + kBN - 1) / kBN);
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / tiles, M / 256)));
+// Slices of k: as many as fill the four work-groups that a compute unit holds, of at least eight slabs each.
+int f32_slices(int M, int N, int K) {
+  const int64_t tiles = (static_cast<int64_t>(M) + kTile - 1) / kTile * ((static_cast<int64_t>(N) + kTile - 1) / kTile);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, K / (8 * kBK))));
+}
+size_t slice_bytes(int M, int N, int K) {
+  const int s = f32_slices(M, N, K);
+  return s > 1 ? align256(static_cast<size_t>(s) * M * N * sizeof(float)) : 0;
+}
+// C = A B^T (+ bias), in slices where that pays
+template <bool A_ALONG, bool B_ALONG>
+hipError_t product(F32Args g, float *part, hipStream_t st) {
+  int s = f32_slices(g.M, g.N, g.K);
+  g.k_per = ((g.K + s - 1) / s + kBK - 1) / kBK * kBK;
+  s = (g.K + g.k_per - 1) / g.k_per;
+  float *out = g.out;
+  if (s > 1) {
+    g.out = part;
+    g.slice = static_cast<int64_t>(g.M) * g.N;
+  }
+  const hipError_t e = launch<kPlain, false, A_ALONG, B_ALONG>(g, s, st);
+  return e == hipSuccess && s > 1 ? launch_partial_reduce(part, out, s, g.slice, g.slice, st) : e;
 }
 int sum_slabs(int M) { return (M + kSumRows - 1) / kSumRows; }
 
@@ -206,36 +236,26 @@ hipError_t launch_gated_f32_in(const GatedIn &in, bool gelu, hipStream_t st) {
   g.keep = static_cast<float *>(in.gu);
   return gelu ? launch<kGate, true, true, true>(g, 1, st) : launch<kGate, false, true, true>(g, 1, st);
 }
-hipError_t launch_gated_f32_out(const float *h, const float *w_out, const float *b_out, float *y, int M, int D, int R, hipStream_t st) {
+size_t gated_f32_product_bytes(int M, int N, int K) { return slice_bytes(M, N, K); }
+hipError_t launch_gated_f32_out(const float *h, const float *w_out, const float *b_out, float *y, int M, int D, int R, float *part, hipStream_t st) {
   F32Args g = whole(h, R, w_out, R, y, M, D, R);
   g.bias = b_out;
-  return launch<kPlain, false, true, true>(g, 1, st);
+  return product<true, true>(g, part, st);
 }
 hipError_t launch_gated_f32_dgate(const float *dy, const float *w_out, const float *gu, float *d_gu, int M, int D, int R, bool gelu, hipStream_t st) {
   F32Args g = whole(dy, D, w_out, R, d_gu, M, R, D);
   g.gu = gu;
   return gelu ? launch<kDGate, true, true, false>(g, 1, st) : launch<kDGate, false, true, false>(g, 1, st);
 }
-hipError_t launch_gated_f32_dx(const float *d_gu, const float *w_in, float *dx, int M, int D, int R, hipStream_t st) {
-  return launch<kPlain, false, true, false>(whole(d_gu, 2 * static_cast<int64_t>(R), w_in, D, dx, M, D, 2 * R), 1, st);
+hipError_t launch_gated_f32_dx(const float *d_gu, const float *w_in, float *dx, int M, int D, int R, float *part, hipStream_t st) {
+  return product<true, false>(whole(d_gu, 2 * static_cast<int64_t>(R), w_in, D, dx, M, D, 2 * R), part, st);
 }
 size_t gated_f32_wgrad_bytes(int M, int N, int K) {
-  const int s = wgrad_slices(M, N, K);
-  const size_t dw = s > 1 ? static_cast<size_t>(s) * N * K : 0, db = static_cast<size_t>(sum_slabs(M)) * N;
-  return align256(std::max(dw, db) * sizeof(float));
+  return std::max(slice_bytes(N, K, M), align256(static_cast<size_t>(sum_slabs(M)) * N * sizeof(float)));
 }
 hipError_t launch_gated_f32_wgrad(const float *dy, const float *x, float *dw, float *db, int M, int N, int K, void *ws, hipStream_t st) {
-  int s = wgrad_slices(M, N, K);
-  F32Args g = whole(dy, N, x, K, dw, N, K, M);
-  g.k_per = ((M + s - 1) / s + kBK - 1) / kBK * kBK;
-  s = (M + g.k_per - 1) / g.k_per;
   float *part = static_cast<float *>(ws);
-  if (s > 1) {
-    g.out = part;
-    g.slice = static_cast<int64_t>(N) * K;
-  }
-  hipError_t e = launch<kPlain, false, false, false>(g, s, st);
-  if (e == hipSuccess && s > 1) e = launch_partial_reduce(part, dw, s, g.slice, g.slice, st);
+  hipError_t e = product<false, false>(whole(dy, N, x, K, dw, N, K, M), part, st);
   if (e != hipSuccess || !db) return e;
   const int slabs = sum_slabs(M);
   if (slabs > 65535) return hipErrorInvalidValue;

@@ -37,6 +37,7 @@ struct GemmArgs {
   // gated feed-forward layer (gated_gemm.hip)
   const float *x_scale, *w_scale;      // e4m3 operands: one factor a row of A, one a row of W
   const void *gu;                      // gradient: the forward's [g | u], act [M, 2N]
+  int k_slabs;                         // slices of k (blockIdx.y): slabs of 64 in each
 };
 
 template <int EPI>
@@ -53,10 +54,11 @@ enum GatedEpilogue {
   kEpiGelu1 = 1,          // + 2: keeps [gate | up] in out2 too, + 4: A and W are e4m3 with scales
   kEpiKeep = 2,
   kEpiE4m3 = 4,
-  EPI_DGATE = 64          // acc = gradient of the hidden layer: out(act) = gradients of [gate | up]; + 1: GELU
+  EPI_DGATE = 64,         // acc = gradient of the hidden layer: out(act) = gradients of [gate | up]; + 1: GELU
+  EPI_SLICE = 96          // out(f32) [slices, M, N] = the sum over a slice of k (gemm_small.inc alone)
 };
 constexpr bool epi_gated(int epi) { return epi >= EPI_GATED && epi < EPI_DGATE; }
-constexpr bool epi_dgate(int epi) { return epi >= EPI_DGATE; }
+constexpr bool epi_dgate(int epi) { return epi >= EPI_DGATE && epi < EPI_SLICE; }
 constexpr bool epi_e4m3(int epi) { return epi_gated(epi) && (epi & kEpiE4m3); }
 
 // Stores of a wave's epilogue over 64 rb rows inside the matrix, or fewer: the persistent kernels' waits let them be in flight.
