@@ -234,7 +234,6 @@ hipError_t attention_bwd_init();
 hipError_t wgrad_init();
 // parameter gradients of up to kWgradMax linear layers at once
 size_t wgrad_ws_bytes(int dtype, const WgradOp *op, int n_op, int M);
-size_t wgrad_rounded_ws_bytes(const WgradOp *op, int n_op, int M);
 hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded = false);
 int layernorm_bwd_slabs(int64_t rows);   // partial rows (of 2 D floats) launch_layernorm_bwd writes
 hipError_t launch_layernorm_bwd(int dtype, const float *x, const void *dy, const float *g, const float *res,

@@ -1,8 +1,8 @@
 // Internal declarations of the gated feed-forward layer: y = (act(x Wg^T + bg) o (x Wu^T + bu)) Wo^T + bo.
-// gated.hip holds the entry points, gated_gemm.hip the bf16 and e4m3 products on tiles, gated_token.hip those of few rows,
-// gated_f32.hip the fp32 path.
+// gated.hip holds the entry points, gated_gemm.hip the bf16 and e4m3 products, gated_f32.hip the fp32 path.
 #pragma once
 
+#include "gated_plan.h"
 #include "gelu.h"
 #include "rows_common.h"
 
@@ -62,16 +62,15 @@ struct GatedIn {                       // x W_in^T and what follows up to the hi
 };
 hipError_t gated_gemm_init();
 hipError_t launch_gated_in(const GatedIn &g, bool gelu, hipStream_t st);
-// the same for few rows, any type (gated_token.hip); rows of x, W_in, h and W_out are multiples of 64 bytes
-hipError_t launch_gated_token_in(int x_dtype, const GatedIn &g, bool gelu, hipStream_t st);
-hipError_t launch_gated_token_out(int dtype, const void *h, const void *w_out, const float *b_out, void *y, int M, int D, int R, hipStream_t st);
-// out [M, N] bf16 = a [M, K] w [N, K]^T (+ bias, may be null), the sum over k cut into slices where one tile a work-group would leave compute units
-// idle; part: gated_slices() M N floats
-int gated_slices(int M, int N, int K);
-hipError_t launch_gated_sliced(const void *a, const void *w, const float *bias, void *out, int M, int N, int K, float *part, hipStream_t st);
-// d_gu [M, 2R] from dy [M, D], the transposed output map wt_out [R, D] and the forward's gu
-hipError_t launch_gated_dgate(const void *dy, const void *wt_out, const void *gu, void *d_gu, int M, int D, int R, bool gelu, hipStream_t st);
-// dst [C, R] (rows ld apart) = src [R, C]^T, bf16, both matrices of the layer in one launch
+// out [M, N] bf16 = a [M, K] times w [N, K] transposed, or w [K, N] (across), + bias (may be null); how: gated_choose_out(); part: how.slices M N floats
+// where how.slices > 1.  other: microseconds that kernels beside the ring cost on top (the ring alone reads w across).
+GatedChoice gated_choose_out(int M, int N, int K, double other);
+hipError_t launch_gated_out(const GatedChoice &how, const void *a, const void *w, bool across, const float *bias, const float *zeros, void *out, int M, int N, int K, float *part,
+                            hipStream_t st);
+// d_gu [M, 2R] from dy [M, D], the output map [D, R] (across) or its transpose [R, D], and the forward's gu
+GatedChoice gated_choose_dgate(int M, int D, int R, double other);
+hipError_t launch_gated_dgate(const GatedChoice &how, const void *dy, const void *w, bool across, const void *gu, void *d_gu, int M, int D, int R, bool gelu, hipStream_t st);
+// wt_in [D, 2R] = w_in^T, wt_out [R, D] = w_out^T in one launch; a destination that is null is left out
 hipError_t launch_gated_transpose(const void *w_in, void *wt_in, const void *w_out, void *wt_out, int D, int R, hipStream_t st);
 
 // fp32, any sizes; see gated_f32.hip.  part: partial sums of the slices of a product [M, N] over K, gated_f32_product_bytes()

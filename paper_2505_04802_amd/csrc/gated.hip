@@ -50,15 +50,23 @@ __global__ __launch_bounds__(256) void gated_zero_kernel(ZeroArgs a) {
 // ------------------------------------------------------------------ workspaces
 static size_t gated_hidden_bytes(int M, int R, int x_dtype) { return align256(static_cast<size_t>(M) * R * (x_dtype == RESLIM_F32 ? 4 : 2)); }
 // partial sums of a product's slices: out [M, N] over K
-static size_t gated_part_bytes(int M, int N, int K, int x_dtype) {
+static size_t gated_part_bytes(int slices, int M, int N) { return slices > 1 ? align256(static_cast<size_t>(slices) * M * N * sizeof(float)) : 0; }
+static size_t gated_out_bytes(int M, int D, int R, int x_dtype) {
   if (M < 1) return 0;
-  if (x_dtype == RESLIM_F32) return gated_f32_product_bytes(M, N, K);
-  const int s = gated_slices(M, N, K);
-  return s > 1 ? align256(static_cast<size_t>(s) * M * N * sizeof(float)) : 0;
+  return x_dtype == RESLIM_F32 ? gated_f32_product_bytes(M, D, R) : gated_part_bytes(gated_choose_out(M, D, R, 0.0).slices, M, D);
+}
+static size_t gated_fwd_bytes(int M, int D, int R, int x_dtype) { return gated_out_bytes(M, D, R, x_dtype) + gated_hidden_bytes(M, R, x_dtype); }
+
+// How the two input gradients of the bf16 path are computed.  The 64 x 64 tiles read the weights as they lie; for the other kernels they are copied
+// transposed first, read and written once at about 4.5 TB/s, after the launch.
+struct GatedBwdPlan { GatedChoice dgate, dx; };
+static GatedBwdPlan gated_bwd_plan(int M, int D, int R) {
+  const double copy = 4e-6 / 4.5 * D * static_cast<double>(R);
+  return {gated_choose_dgate(M, D, R, 2.0 + copy), gated_choose_out(M, D, 2 * R, 2.0 + 2 * copy)};
 }
 struct GatedBwdWs {
   void *d_gu;                  // act [M, 2R]
-  void *wt_in, *wt_out;        // bf16 [D, 2R], [R, D]
+  void *wt_in, *wt_out;        // bf16 [D, 2R], [R, D], or null
   void *part;                  // partial sums of dx
   void *wgrad;                 // partial sums of the parameter gradients
   void *sink_in, *sink_out;    // 2R and D floats: bias gradients that nobody asked for
@@ -74,23 +82,25 @@ static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, int grad_dtype,
   auto take = [&](size_t bytes) { unsigned char *q = p + off; off += align256(bytes); return q; };
   const size_t es = type_bytes(dtype), m = M, d = D, r = R;
   GatedBwdWs w = {};
+  if (M < 1) return w;
   w.d_gu = take(m * 2 * r * es);
-  w.part = take(gated_part_bytes(M, D, 2 * R, dtype));
   if (dtype == RESLIM_BF16) {
-    w.wt_in = take(2 * r * d * 2);
-    w.wt_out = take(r * d * 2);
+    const GatedBwdPlan plan = gated_bwd_plan(M, D, R);
+    w.part = take(gated_part_bytes(plan.dx.slices, M, D));
+    if (plan.dx.kernel != kGatedRing) w.wt_in = take(2 * r * d * 2);
+    if (plan.dgate.kernel != kGatedRing) w.wt_out = take(r * d * 2);
     w.sink_in = take(2 * r * sizeof(float));
     w.sink_out = take(d * sizeof(float));
     WgradOp op[2];
     gated_ops(op, nullptr, nullptr, nullptr, nullptr, D, R);
-    w.wgrad = take(M < 1 ? 0 : grad_dtype == RESLIM_BF16 ? wgrad_rounded_ws_bytes(op, 2, M) : wgrad_ws_bytes(RESLIM_BF16, op, 2, M));
+    w.wgrad = take(wgrad_ws_bytes(RESLIM_BF16, op, 2, M));
   } else {
+    w.part = take(gated_f32_product_bytes(M, D, 2 * R));
     w.wgrad = take(std::max(gated_f32_wgrad_bytes(M, 2 * R, D), gated_f32_wgrad_bytes(M, D, R)));
   }
   w.total = off;
   return w;
 }
-static size_t gated_fwd_bytes(int M, int D, int R, int x_dtype) { return gated_part_bytes(M, D, R, x_dtype) + gated_hidden_bytes(M, R, x_dtype); }
 
 // ------------------------------------------------------------------ checks
 static int gated_shape(const char *fn, int rows, int D, int R, int x_dtype) {
@@ -122,27 +132,12 @@ static int gated_room(const char *fn, const void *ws, size_t ws_bytes, size_t ne
   return refuse(RESLIM_EWORKSPACE, fn, "workspace null, not 256-byte aligned or smaller than the workspace query says");
 }
 
-// Few rows: the weights' bytes bound both products, and streaming them past the token rows beats tiles, bf16 at 4096 x 10,944 (both products, us):
-// 1 row 67 against 171 (79 with the output map in slices), 8 rows 76 against 79, 16 rows 89 against 81.  The fp32 tiles have no persistent kernel
-// behind them: up to 64 rows.
-static bool gated_few(int x_dtype, int M, int D, int R, const GatedIn &in, const reslim_gated_mlp_weights *w) {
-  const int es = x_dtype == RESLIM_F32 ? 4 : 2;
-  if (M > (x_dtype == RESLIM_F32 ? 64 : 8) || D * type_bytes(x_dtype) % 64 || R * es % 64) return false;
-  return x_dtype != RESLIM_F32 || (aligned(in.x, 16) && aligned(in.w_in, 16) && aligned(in.h, 16) && aligned(w->w_out, 16));
-}
-
 static hipError_t gated_forward(const GatedIn &in, const reslim_gated_mlp_weights *w, int x_dtype, bool gelu, void *y, void *part, const float *zeros, hipStream_t st) {
-  const int dtype = x_dtype == RESLIM_F32 ? RESLIM_F32 : RESLIM_BF16;
-  if (gated_few(x_dtype, in.M, in.D, in.R, in, w)) {
-    const hipError_t e = launch_gated_token_in(x_dtype, in, gelu, st);
-    return e == hipSuccess ? launch_gated_token_out(dtype, in.h, w->w_out, w->b_out, y, in.M, in.D, in.R, st) : e;
-  }
   const bool f32 = x_dtype == RESLIM_F32;
   const hipError_t e = f32 ? launch_gated_f32_in(in, gelu, st) : launch_gated_in(in, gelu, st);
   if (e != hipSuccess) return e;
   if (f32) return launch_gated_f32_out(static_cast<const float *>(in.h), static_cast<const float *>(w->w_out), w->b_out, static_cast<float *>(y), in.M, in.D, in.R, static_cast<float *>(part), st);
-  if (gated_slices(in.M, in.D, in.R) > 1) return launch_gated_sliced(in.h, w->w_out, w->b_out, y, in.M, in.D, in.R, static_cast<float *>(part), st);
-  return launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, in.h, w->w_out, w->b_out ? w->b_out : zeros, y, in.D, nullptr, 0, in.M, in.D, in.R, st);
+  return launch_gated_out(gated_choose_out(in.M, in.D, in.R, 0.0), in.h, w->w_out, false, w->b_out, zeros, y, in.M, in.D, in.R, static_cast<float *>(part), st);
 }
 
 }  // namespace reslim
@@ -171,7 +166,7 @@ extern "C" int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const r
   if (rows == 0) return RESLIM_OK;
   const float *zeros = nullptr;
   hipError_t e = gated_ready(&zeros);
-  unsigned char *h = static_cast<unsigned char *>(workspace) + gated_part_bytes(rows, D, R, x_dtype);
+  unsigned char *h = static_cast<unsigned char *>(workspace) + gated_out_bytes(rows, D, R, x_dtype);
   const GatedIn in = {x, w->w_in, x_scale, w->in_scale, w->b_in, nullptr, h, rows, D, R};
   if (e == hipSuccess) e = gated_forward(in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
@@ -242,11 +237,11 @@ extern "C" int reslim_gated_mlp_bwd(const void *x, const void *gu, const void *h
     if (e == hipSuccess) e = launch_gated_f32_wgrad(f(dy), f(h), o(grads->w_out), o(grads->b_out), rows, D, R, ws.wgrad, st);
     return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
   }
-  e = launch_gated_transpose(w->w_in, ws.wt_in, w->w_out, ws.wt_out, D, R, st);
-  if (e == hipSuccess) e = launch_gated_dgate(dy, ws.wt_out, gu, ws.d_gu, rows, D, R, gelu, st);
+  const GatedBwdPlan plan = gated_bwd_plan(rows, D, R);
+  e = launch_gated_transpose(w->w_in, dx ? ws.wt_in : nullptr, w->w_out, ws.wt_out, D, R, st);
+  if (e == hipSuccess) e = launch_gated_dgate(plan.dgate, dy, ws.wt_out ? ws.wt_out : w->w_out, !ws.wt_out, gu, ws.d_gu, rows, D, R, gelu, st);
   if (e == hipSuccess && dx)
-    e = gated_slices(rows, D, 2 * R) > 1 ? launch_gated_sliced(ws.d_gu, ws.wt_in, nullptr, dx, rows, D, 2 * R, static_cast<float *>(ws.part), st)
-                                         : launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, ws.d_gu, ws.wt_in, zeros, dx, D, nullptr, 0, rows, D, 2 * R, st);
+    e = launch_gated_out(plan.dx, ws.d_gu, ws.wt_in ? ws.wt_in : w->w_in, !ws.wt_in, nullptr, zeros, dx, rows, D, 2 * R, static_cast<float *>(ws.part), st);
   if (e == hipSuccess) {
     WgradOp op[2];
     gated_ops(op, ws.d_gu, x, dy, h, D, R);

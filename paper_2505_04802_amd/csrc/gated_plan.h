@@ -1,0 +1,46 @@
+// Which kernel a product of the gated feed-forward layer gets, and into how many slices its sum is cut (gated_gemm.hip).  Arithmetic
+// only: the CPU test compiles it too and holds the choice against measured times.
+#pragma once
+
+#include "gemm_plan.h"
+
+namespace reslim {
+
+constexpr int kGatedRing = 1;      // 64 x 64 tiles; beside the kernels of GemmKernel
+struct GatedChoice {
+  int kernel, slices;              // slices > 1: the ring or the 128 x 128 tiles
+  double us;
+};
+
+// The smallest of the estimates of gemm_times and of those for the 64 x 64 tiles, in microseconds beside what every launch costs.  A slab of these takes
+// a work-group 0.26 us, its latency over the three in flight, while two lie on a compute unit, and a compute unit 0.27, what it draws
+// from L2 for one.  Slices of k make more work-groups of shorter sums, at the price of a second launch and of partial sums that are read
+// again.  gemm_times is fitted to products whose weights lie in a cache; a model's come from memory, and where every work-group has one tile a slab
+// then takes a persistent kernel 0.8 us (128 x 256) and 1.35 (256 x 256): 64 x 4096 x 10,944 140 us instead of 79.  N: rows of W that are read
+// (both matrices of a gated product); cols: columns of the result; slabs: K in slabs of 128 bytes a row; other: what the kernels
+// beside the ring cost on top (copies of weights that it does without).
+inline GatedChoice gated_choose(int M, int N, int cols, int slabs, GemmEpi epi, int cus, bool sliceable, bool e4m3, double other) {
+  constexpr double ring_epi[] = {0.8, 1.0, 1.5, 1.0, 2.0};
+  const GemmTimes g = gemm_times(M, N, slabs * 64, epi, cus);
+  auto count = [&](int bm, int bn) { return static_cast<double>((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  const double tiles = count(64, 64), mid = count(128, 128);
+  GatedChoice best = {kGemm256x256, 1, (count(256, 256) <= cus ? std::max(g.pp2, slabs * 1.35) : g.pp2) + other};
+  auto offer = [&](int kernel, int slices, double us) {
+    if (us < best.us) best = {kernel, slices, us};
+  };
+  offer(kGemm128x256, 1, (count(128, 256) <= cus ? std::max(g.pp1, slabs * 0.8) : g.pp1) + other);
+  if (!e4m3) offer(kGemm128, 1, g.small + other);
+  for (int s = 1; s <= 32 && (s == 1 || slabs / s >= 4); ++s) {
+    if (s > 1 && !sliceable) break;
+    const int per = (slabs + s - 1) / s, n = (slabs + per - 1) / per;
+    const double rounds = std::ceil(tiles * n / (2.0 * cus)), add = n > 1 ? 2.4 + 5e-6 / 4.5 * n * M * static_cast<double>(cols) : 0.0;
+    offer(kGatedRing, n, 0.5 + std::max(rounds * per * 0.26, tiles * n * per * 0.27 / cus) + rounds * ring_epi[epi] + add);
+    if (s > 1 && mid * n <= 3.0 * cus) {                   // 128 x 128 tiles, up to three on a compute unit
+      const double ws = mid * n / cus, fs = std::min(1.0, std::max(0.0, (0.62 * std::ceil(ws) + 0.38 * ws - 1.0) / 2.0));
+      offer(kGemm128, n, per * (0.73 + 1.07 * fs) + 5.99 * (0.12 + 0.88 * fs) + add + other);
+    }
+  }
+  return best;
+}
+
+}  // namespace reslim

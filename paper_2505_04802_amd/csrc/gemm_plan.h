@@ -26,7 +26,8 @@ enum GemmEpi { kEpiAct, kEpiGelu, kEpiTwo, kEpiF32, kEpiStream };
 // persistent launch that starts on all CUs at once lowers the clock by 7 % for the launches around it, short as it may be; one
 // product of 16,200 x 512 x 512 in a forward of 0.70 ms that has no other costs 0.05 ms there, and saves 2 us.  Long products run at
 // the power limit anyway.
-inline GemmKernel gemm_choose(int M, int N, int K, GemmEpi epi, int num_cus) {
+struct GemmTimes { double small, pp2, pp1; };      // one tile per work-group; persistent 256 x 256, 128 x 256
+inline GemmTimes gemm_times(int M, int N, int K, GemmEpi epi, int num_cus) {
   constexpr double small_epi[] = {3.3, 3.32, 5.4, 5.99, 6.17}, pp2_epi[] = {4.81, 9.5, 13.97, 6.33, 11.12}, pp1_epi[] = {3.72, 5.25, 8.53, 3.41, 6.76};
   const double nk = K / 64, cus = num_cus;
   auto tiles = [&](int bm, int bn) { return static_cast<double>((M + bm - 1) / bm) * ((N + bn - 1) / bn) / cus; };      // per CU
@@ -37,7 +38,11 @@ inline GemmKernel gemm_choose(int M, int N, int K, GemmEpi epi, int num_cus) {
   const double c2 = promise(2.46 + std::ceil(w2) * (nk * (1.08 + 0.10 * f2) + pp2_epi[epi] * (0.36 + 0.64 * f2)), w2);
   const double c1 = promise(0.34 + std::ceil(w1) * (nk * (0.43 + 0.30 * f1) + pp1_epi[epi]), w1);
   const double cs = std::max(1.0, ws / 3.0) * (nk * (0.73 + 1.07 * fs) + small_epi[epi] * (0.12 + 0.88 * fs));
-  return cs <= c1 && cs <= c2 ? kGemm128 : c1 < c2 ? kGemm128x256 : kGemm256x256;
+  return {cs, c2, c1};
+}
+inline GemmKernel gemm_choose(int M, int N, int K, GemmEpi epi, int num_cus) {
+  const GemmTimes t = gemm_times(M, N, K, epi, num_cus);
+  return t.small <= t.pp1 && t.small <= t.pp2 ? kGemm128 : t.pp1 < t.pp2 ? kGemm128x256 : kGemm256x256;
 }
 
 // fp32 path: whether a product M x N x K normalises its rows itself (gemm_f32_kernel with LN) instead of after a launch of its own.

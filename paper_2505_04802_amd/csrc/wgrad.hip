@@ -105,7 +105,8 @@ __device__ __forceinline__ void wgrad_wait_vm_lgkm0() {
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
 }
 
-template <int RB>
+// T: float, or bf16 for a single slice whose gradients are of the weights' own type
+template <int RB, class T>
 __global__ __launch_bounds__(512, 2) void wgrad_bf16_kernel(WgradArgs a) {
   constexpr int TN = 128 * RB, TK = 256, BM = 64;
   constexpr int kRowN = 128 * RB, kRowK = 256;                         // bytes of a half-tile row in LDS
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(512, 2) void wgrad_bf16_kernel(WgradArgs a) {
 
   // ---- store: accumulator register r of lane (l32, hi) is row 8 (r / 4) + 4 hi + r % 4, column l32
   auto store = [&](auto edge) {
-    float *out = op.out + static_cast<size_t>(split) * a.split_stride + static_cast<size_t>(n0) * op.K + k0;
+    T *out = reinterpret_cast<T *>(op.out) + static_cast<size_t>(split) * a.split_stride + static_cast<size_t>(n0) * op.K + k0;
 #pragma unroll
     for (int nh = 0; nh < 2; ++nh)
 #pragma unroll
@@ -345,10 +346,10 @@ __global__ __launch_bounds__(512, 2) void wgrad_bf16_kernel(WgradArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int n = nh * 64 * RB + (wm * RB + i) * 32 + 8 * (r / 4) + 4 * hi + (r % 4);
-          float *row = out + static_cast<size_t>(n) * op.K + wn * 32 + l32;
+          T *row = out + static_cast<size_t>(n) * op.K + wn * 32 + l32;
 #pragma unroll
           for (int kh = 0; kh < 2; ++kh)
-            if (!decltype(edge)::value || (n0 + n < op.N && k0 + kh * 128 + wn * 32 + l32 < op.K)) row[kh * 128] = acc[RB * nh + i][kh][r];
+            if (!decltype(edge)::value || (n0 + n < op.N && k0 + kh * 128 + wn * 32 + l32 < op.K)) Act<T>::store(row + kh * 128, acc[RB * nh + i][kh][r]);
         }
   };
   if (n0 + TN <= op.N && k0 + TK <= op.K) store(std::integral_constant<bool, false>{});
@@ -364,8 +365,8 @@ __global__ __launch_bounds__(512, 2) void wgrad_bf16_kernel(WgradArgs a) {
         if (hi == 0) sm[wn * TN + nh * 64 * RB + (wm * RB + i) * 32 + l32] = v;
       }
     __syncthreads();
-    float *ob = op.out_b + static_cast<size_t>(split) * a.split_stride;
-    if (t < TN && n0 + t < op.N) ob[n0 + t] = (sm[t] + sm[TN + t]) + (sm[2 * TN + t] + sm[3 * TN + t]);
+    T *ob = reinterpret_cast<T *>(op.out_b) + static_cast<size_t>(split) * a.split_stride;
+    if (t < TN && n0 + t < op.N) Act<T>::store(ob + n0 + t, (sm[t] + sm[TN + t]) + (sm[2 * TN + t] + sm[3 * TN + t]));
   }
 }
 
@@ -387,8 +388,10 @@ hipError_t wgrad_init() {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&g_wgrad_cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<1>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<1>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<2>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<2>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<1, float>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<1>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<1, bf16_t>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<1>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<2, float>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<2>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void *>(&wgrad_bf16_kernel<2, bf16_t>), hipFuncAttributeMaxDynamicSharedMemorySize, wgrad_lds<2>());
   return e;
 }
 
@@ -464,13 +467,9 @@ size_t wgrad_ws_bytes(int dtype, const WgradOp *op, int n_op, int M) {
   return p.splits > 1 ? align256(static_cast<size_t>(p.splits) * wgrad_slice(op, n_op) * sizeof(float)) : 0;
 }
 
-size_t wgrad_rounded_ws_bytes(const WgradOp *op, int n_op, int M) {
-  return align256(static_cast<size_t>(wgrad_plan(op, n_op, M).splits) * wgrad_slice(op, n_op) * sizeof(float));
-}
-
-// rounded: the gradients are bf16 (dw and db point at bf16), written by the sum over the slices, also of a single one
+// rounded: the gradients are bf16 (dw and db point at bf16), rounded by the sum over the slices, or by the only slice
 static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded) {
-  const bool summed = rounded || p.splits > 1;
+  const bool summed = p.splits > 1;
   if (summed && !ws) return hipErrorInvalidValue;
   WgradArgs a = {};
   WgradReduceArgs r = {};
@@ -501,8 +500,11 @@ static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n
   a.tiles = tiles;
   a.m_per_split = p.m_per_split;
   const dim3 grid(tiles * p.splits);
-  if (p.kind == kWgrad256) wgrad_bf16_kernel<2><<<grid, dim3(512), wgrad_lds<2>(), st>>>(a);
-  else wgrad_bf16_kernel<1><<<grid, dim3(512), wgrad_lds<1>(), st>>>(a);
+  const bool two = p.kind == kWgrad256, direct = rounded && !summed;
+  if (two && direct) wgrad_bf16_kernel<2, bf16_t><<<grid, dim3(512), wgrad_lds<2>(), st>>>(a);
+  else if (two) wgrad_bf16_kernel<2, float><<<grid, dim3(512), wgrad_lds<2>(), st>>>(a);
+  else if (direct) wgrad_bf16_kernel<1, bf16_t><<<grid, dim3(512), wgrad_lds<1>(), st>>>(a);
+  else wgrad_bf16_kernel<1, float><<<grid, dim3(512), wgrad_lds<1>(), st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !summed) return e;
   r.partial = static_cast<const float4 *>(ws);
