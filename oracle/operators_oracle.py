@@ -40,8 +40,8 @@ def rmsnorm_bwd(s, dy, gamma, eps, d_sum):
         bound = bound + 2 * E * d_sum.double().abs()
     dgamma = (dy * h).sum(0)
     rows = s.shape[0]
-    # a work-group adds up to ceil(rows / 1024) rows one by one, then at most 1024 partial sums follow
-    serial = math.ceil(rows / 1024) + 64 + min(rows, 1024) / 8
+    # a work-group adds up to ceil(rows / 768) rows one by one, then at most 768 partial sums follow
+    serial = math.ceil(rows / 768) + 64 + min(rows, 768) / 8
     return dx, dgamma, bound, (32 + serial) * E * (dy * h).abs().sum(0)
 
 

@@ -88,6 +88,39 @@ template <int V> struct Piece<e4m3_t, V> {
   }
 };
 
+// The same elements as they lie in memory, to be held until they are used.
+template <class T, int V> struct Held {
+  static constexpr int kWords = (V * static_cast<int>(sizeof(T)) + 3) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (kWords % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const u32x4_row r = *reinterpret_cast<const u32x4_row *>(reinterpret_cast<const uint32_t *>(p) + i);
+        w[i] = r[0]; w[i + 1] = r[1]; w[i + 2] = r[2]; w[i + 3] = r[3];
+      }
+    } else if constexpr (kWords == 2) {
+      const u32x2_row r = *reinterpret_cast<const u32x2_row *>(p);
+      w[0] = r[0]; w[1] = r[1];
+    } else if constexpr (sizeof(T) == 4) {
+      w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t *>(p);
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+
+// ... and as floats
+template <class T, int V> struct Loaded {
+  float v[V];
+  __device__ __forceinline__ void load(const T *p) { Piece<T, V>::load(p, v); }
+  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+
 // Sum (or maximum) over the NT threads that share a row, the same value in all of them.  box: NT / 64 floats of LDS that nothing
 // else uses until every thread is past the call after next (two boxes taken in turn).
 template <int NT, bool MAX>
@@ -105,6 +138,31 @@ __device__ __forceinline__ float row_all(float s, float *box) {
     for (int w = 1; w < NT / 64; ++w) s = MAX ? fmaxf(s, box[w]) : s + box[w];
   }
   return s;
+}
+
+// Two sums at once, over one barrier; box: 2 NT / 64 floats
+template <int NT>
+__device__ __forceinline__ void row_sum2(float &a, float &b, float *box) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    a += __shfl_xor(a, m);
+    b += __shfl_xor(b, m);
+  }
+  if constexpr (NT > 64) {
+    constexpr int W = NT / 64;
+    if ((threadIdx.x & 63) == 0) {
+      box[threadIdx.x >> 6] = a;
+      box[W + (threadIdx.x >> 6)] = b;
+    }
+    __syncthreads();
+    a = box[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) a += box[w];
+    if constexpr (W == 16) __builtin_amdgcn_sched_barrier(0);      // sixteen values at a time
+    b = box[W];
+#pragma unroll
+    for (int w = 1; w < W; ++w) b += box[W + w];
+  }
 }
 
 // An entry point without a context refuses: the text goes to reslim_last_error(NULL).  Throws nothing.

@@ -49,7 +49,7 @@ def test_rmsnorm_bwd_refusals(kw, code):
 def test_rmsnorm_workspace():
     assert B.reslim_rmsnorm_bwd_workspace_bytes(0, 100) == 0
     assert B.reslim_rmsnorm_bwd_workspace_bytes(3, 100) == 1280                       # 1200 bytes to the next 256
-    assert B.reslim_rmsnorm_bwd_workspace_bytes(10 ** 6, 4096) == 1024 * 4096 * 4
+    assert B.reslim_rmsnorm_bwd_workspace_bytes(10 ** 6, 4096) == 768 * 4096 * 4
     for rows, D in ((-1, 4), (1, 0), (1, 16385)):
         with pytest.raises(B.ReslimError):
             B.reslim_rmsnorm_bwd_workspace_bytes(rows, D)
