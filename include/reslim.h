@@ -616,8 +616,8 @@ int reslim_rmsnorm_bwd(const void *sum, const void *dy, const float *gamma, floa
  *             Only the `heads` rotated heads are written
  *   positions int32 [axes, period];  freq double [rot / 2];  dtype RESLIM_F32 or RESLIM_BF16
  * rot: a multiple of 2 * axes, at most dh; dh even, at most 1024; x_stride, out_stride >= heads * dh.  Interleaved bf16 pairs
- * start on 4 bytes.  Full speed: pieces of 16 bytes that neither a head's start, rot (rot / 2 for pairs of halves) nor
- * dh cuts; other sizes go pair by pair.
+ * start on 4 bytes.  Fastest where 16-byte pieces start in every head and neither rot (rot / 2 for pairs of halves) nor dh
+ * ends inside one; otherwise pieces are as narrow as that takes.
  * reslim_rotary_bwd is the gradient, the same turn backwards: d_out in, d_x out (in place allowed). */
 enum { RESLIM_ROTARY_INTERLEAVED = 0, RESLIM_ROTARY_HALVES = 1 };
 int reslim_rotary_fwd(const void *x, void *out, const int32_t *positions, const double *freq, int64_t tokens, int64_t x_stride,

@@ -35,39 +35,34 @@ __device__ __forceinline__ void turn(double angle, float amplitude, float sign, 
   s = amplitude * sign * sn;
 }
 
-// V: features a thread moves at once; HALVES: pairs (j, j + rot / 2)
+// V: features of a piece; HALVES: pairs (j, j + rot / 2), two pieces a thread.  Threads behind the turning pieces copy, on the same path (the
+// other one would cost every wave the latency of both): 25,986 x 20 heads of 128, half of each turning, 81 us with a path of their own.
 template <class T, int V, bool HALVES>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  constexpr int NP = HALVES ? V : V / 2;       // pairs of a piece
+  constexpr int NP = HALVES ? V : V / 2;       // pairs of a thread
   const int per_token = a.pieces * a.lanes;
   const int tpb = per_token < 256 ? 256 / per_token : 1;      // tokens of a work-group
   const int slot = threadIdx.x / per_token;
   const int64_t token = static_cast<int64_t>(blockIdx.x) * tpb + slot;
   if (slot >= tpb || token >= a.tokens) return;
   const int within = threadIdx.x % per_token;
-  const int turning = a.rot / 2 / NP;          // pieces that turn; the ones behind them are copied
+  const int turning = a.rot / 2 / NP;
   const int64_t at = token % a.period;
+  const T *x = static_cast<const T *>(a.x) + token * a.x_stride;
+  T *o = static_cast<T *>(a.out) + token * a.out_stride;
   for (int u = within; u < per_token; u += 256) {      // more than one round only where a head has more than 256 pieces
     const int piece = u % a.pieces, lane = u / a.pieces;
-    const T *x = static_cast<const T *>(a.x) + token * a.x_stride;
-    T *o = static_cast<T *>(a.out) + token * a.out_stride;
-    if (piece >= turning) {
-      const int k = a.rot + (piece - turning) * V;
-      for (int h = lane; h < a.heads; h += a.lanes) {
-        float v[V];
-        Piece<T, V>::load(x + h * a.dh + k, v);
-        Piece<T, V>::store(o + h * a.dh + k, v);
-      }
-      continue;
-    }
+    const bool turns = piece < turning;
     float c[NP], s[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int j = piece * NP + i;
+      const int j = turns ? piece * NP + i : 0;
       const int axis = 2 * j * a.axes / a.rot;           // 0, or 1 in the second half of the pairs
       turn(static_cast<double>(a.positions[axis * a.period + at]) * a.freq[j], a.amplitude, a.sign, c[i], s[i]);
     }
-    const int k0 = HALVES ? piece * V : 2 * piece * NP, k1 = k0 + a.rot / 2;
+    const int k0 = turns ? piece * (HALVES ? V : 2 * NP) : a.rot + (piece - turning) * (HALVES ? 2 * V : V);
+    const int k1 = turns ? k0 + a.rot / 2 : k0 + V;
+    const bool two = HALVES && k1 < a.dh;                // the last copied piece may be single
     constexpr int G = 4;                       // heads whose loads are in flight together
     for (int h0 = lane; h0 < a.heads; h0 += G * a.lanes) {
       float p[G][V], q[G][HALVES ? V : 1];
@@ -76,30 +71,26 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
         const int h = h0 + g * a.lanes;
         if (h < a.heads) {
           Piece<T, V>::load(x + h * a.dh + k0, p[g]);
-          if constexpr (HALVES) Piece<T, V>::load(x + h * a.dh + k1, q[g]);
+          if constexpr (HALVES) {
+            if (two) Piece<T, V>::load(x + h * a.dh + k1, q[g]);
+          }
         }
       }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const int h = h0 + g * a.lanes;
         if (h >= a.heads) break;
-        if constexpr (HALVES) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float u0 = p[g][i], u1 = q[g][i];
-            p[g][i] = u0 * c[i] - u1 * s[i];
-            q[g][i] = u0 * s[i] + u1 * c[i];
-          }
-          Piece<T, V>::store(o + h * a.dh + k1, q[g]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < NP; ++i) {
-            const float u0 = p[g][2 * i], u1 = p[g][2 * i + 1];
-            p[g][2 * i] = u0 * c[i] - u1 * s[i];
-            p[g][2 * i + 1] = u0 * s[i] + u1 * c[i];
-          }
+        for (int i = 0; i < NP; ++i) {
+          float &f0 = HALVES ? p[g][i] : p[g][2 * i], &f1 = HALVES ? q[g][HALVES ? i : 0] : p[g][HALVES ? 0 : 2 * i + 1];
+          const float u0 = f0, u1 = f1;
+          f0 = turns ? u0 * c[i] - u1 * s[i] : u0;
+          f1 = turns ? u0 * s[i] + u1 * c[i] : u1;
         }
         Piece<T, V>::store(o + h * a.dh + k0, p[g]);
+        if constexpr (HALVES) {
+          if (two) Piece<T, V>::store(o + h * a.dh + k1, q[g]);
+        }
       }
     }
   }
@@ -107,8 +98,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
 
 template <class T, int V, bool HALVES>
 static hipError_t launch_rotary_v(RotaryArgs a, hipStream_t st) {
-  const int np = HALVES ? V : V / 2;
-  a.pieces = a.rot / 2 / np + (a.copy ? (a.dh - a.rot) / V : 0);
+  const int np = HALVES ? V : V / 2, copied = HALVES ? 2 * V : V;
+  a.pieces = a.rot / 2 / np + (a.copy ? (a.dh - a.rot + copied - 1) / copied : 0);
   // An angle serves the heads that a thread walks through; threads over the heads are added while the launch leaves the
   // chip without eight waves on a compute unit, down to one head a thread.
   int lanes = (a.heads + 7) / 8;
@@ -123,14 +114,15 @@ static hipError_t launch_rotary_v(RotaryArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <class T>
-static hipError_t launch_rotary(const RotaryArgs &a, bool halves, hipStream_t st) {
-  constexpr int V = 16 / sizeof(T);
-  // 16-byte pieces where they start on 16 bytes and neither the turning part nor what is copied ends inside one
-  const bool whole = aligned(a.x, 16) && aligned(a.out, 16) && a.dh % V == 0 && a.x_stride % V == 0 && a.out_stride % V == 0 && a.rot % (halves ? 2 * V : V) == 0;
-  if (halves) return whole ? launch_rotary_v<T, V, true>(a, st) : launch_rotary_v<T, 1, true>(a, st);
-  // pairs element by element need an even head, or the copied part does not divide into pairs
-  return whole ? launch_rotary_v<T, V, false>(a, st) : launch_rotary_v<T, 2, false>(a, st);
+// The widest pieces, up to 16 bytes, that start on their own size in every head and that neither the turning part (either half of it where
+// pairs are halves) nor the head ends inside.  With single elements 25,986 x 20 heads of 96, 24 of them turning as halves, took 117 us.
+template <class T, bool HALVES, int V>
+static hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st) {
+  if constexpr (V > (HALVES ? 1 : 2)) {
+    const bool starts = aligned(a.x, V * sizeof(T)) && aligned(a.out, V * sizeof(T)) && a.dh % V == 0 && a.x_stride % V == 0 && a.out_stride % V == 0;
+    if (!starts || a.rot % (HALVES ? 2 * V : V)) return launch_rotary<T, HALVES, V / 2>(a, st);
+  }
+  return launch_rotary_v<T, V, HALVES>(a, st);
 }
 
 static int rotary_impl(const char *fn, const void *x, void *out, const int32_t *positions, const double *freq, int64_t tokens, int64_t x_stride, int64_t out_stride,
@@ -153,7 +145,8 @@ static int rotary_impl(const char *fn, const void *x, void *out, const int32_t *
   RotaryArgs a = {x, out, positions, freq, tokens, x_stride, out_stride, period, heads, dh, rot, axes, 0, 0, x != out, amplitude, sign};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const bool halves = layout == RESLIM_ROTARY_HALVES;
-  const hipError_t e = dtype == RESLIM_BF16 ? launch_rotary<bf16_t>(a, halves, st) : launch_rotary<float>(a, halves, st);
+  const hipError_t e = dtype == RESLIM_BF16 ? (halves ? launch_rotary<bf16_t, true, 8>(a, st) : launch_rotary<bf16_t, false, 8>(a, st))
+                                            : (halves ? launch_rotary<float, true, 4>(a, st) : launch_rotary<float, false, 4>(a, st));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
 }
 
