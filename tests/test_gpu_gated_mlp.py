@@ -71,9 +71,12 @@ def _near(got, want, bound, dtype, name):
 SIZES = [(1, 64, 64), (2, 128, 192), (16, 256, 704), (17, 64, 320), (31, 320, 832), (33, 192, 64), (64, 512, 1344), (65, 128, 256), (127, 1024, 2752), (129, 320, 192),
          (197, 320, 832), (256, 64, 128), (300, 1088, 1472), (515, 448, 1216)]
 
+# sizes for the kernels beside the 64 x 64 tiles, and for slices of k
+LARGE = [(400, 1024, 2752), (1001, 1024, 2752), (1300, 1024, 2752), (590, 2048, 5504), (2030, 1024, 2752), (4100, 1024, 2752), (100, 4096, 10944), (999, 2048, 5504)]
+
 
 @pytest.mark.parametrize("gate", ["silu", "gelu"])
-@pytest.mark.parametrize("rows,D,R", SIZES)
+@pytest.mark.parametrize("rows,D,R", SIZES + LARGE)
 def test_forward_bf16(rows, D, R, gate):
     for bias in (False, True):
         x, _, w = _case(rows, D, R, H, bias)
@@ -88,7 +91,8 @@ def test_forward_bf16(rows, D, R, gate):
 
 
 @pytest.mark.parametrize("gate", ["silu", "gelu"])
-@pytest.mark.parametrize("rows,D,R", [(1, 128, 64), (3, 256, 704), (16, 512, 320), (40, 128, 192), (64, 1024, 2752), (130, 384, 832), (257, 640, 1216), (1000, 256, 128)])
+@pytest.mark.parametrize("rows,D,R", [(1, 128, 64), (3, 256, 704), (16, 512, 320), (40, 128, 192), (64, 1024, 2752), (130, 384, 832), (257, 640, 1216), (1000, 256, 128),
+                                       (700, 2048, 5504), (2030, 1024, 2752)])
 def test_forward_e4m3(rows, D, R, gate):
     for bias in (False, True):
         x, xs, w = _case(rows, D, R, H, bias, Q)
@@ -98,7 +102,7 @@ def test_forward_e4m3(rows, D, R, gate):
 
 @pytest.mark.parametrize("gate", ["silu", "gelu"])
 @pytest.mark.parametrize("gt", [H, F], ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows,D,R", SIZES)
+@pytest.mark.parametrize("rows,D,R", SIZES + LARGE)
 def test_backward_bf16(rows, D, R, gt, gate):
     x, _, w = _case(rows, D, R, H, True)
     gu, h, _ = _train(x, w, gate)
