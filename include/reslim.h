@@ -573,7 +573,8 @@ int reslim_asc_forward(reslim_ctx *ctx, const reslim_asc_plan *plan, const float
  * pointers on the current device unless stated; tensors are contiguous row-major unless a stride is given; work is enqueued
  * on hip_stream, nothing is allocated or synchronised, and calls with buffers of their own may overlap.  Results are
  * deterministic.  Sums, statistics and products are fp32 (angles 64-bit), results are rounded once.  rows = 0 (tokens = 0)
- * is allowed: nothing is written but parameter gradients, which become zero.  A refusal enqueues nothing; its text is at
+ * is allowed: nothing is written but parameter gradients, which become zero.  Outputs must not overlap inputs or each other
+ * but where "in place" is said.  A refusal enqueues nothing; its text is at
  * reslim_last_error(NULL).  Errors: RESLIM_EINVAL (null, type, alignment, value), RESLIM_ESHAPE, RESLIM_EWORKSPACE (null,
  * not 256-byte aligned, too small), RESLIM_EHIP. ---- */
 

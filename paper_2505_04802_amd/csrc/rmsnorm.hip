@@ -8,6 +8,7 @@
 // of a row is issued before the first is used, and 16 bytes of the stream is what a thread takes at a time.  Sums are
 // fp32 in an order that depends on the row's width and alignment alone, so a row's result does not depend on the
 // others.  s is normalised before it is rounded to the stream's type.
+#include <algorithm>
 #include <type_traits>
 
 #include "rows_common.h"
@@ -233,12 +234,22 @@ static void norm_shape(int D, F &&f) {
 }
 
 template <class S, class A, class Y, int V>
-static hipError_t launch_norm_v(const NormArgs &a, hipStream_t st) {
+static hipError_t launch_norm_v(NormArgs a, hipStream_t st) {
+  auto past = [](auto *p, int64_t bytes) { return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + bytes) : p; };
+  hipError_t e = hipSuccess;
   norm_shape<V>(a.D, [&](auto nt, auto nc) {
-    constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value, RPB = NT < 256 ? 256 / NT : 1;
-    rmsnorm_kernel<S, A, Y, V, NT, NC><<<dim3(static_cast<unsigned>((a.rows + RPB - 1) / RPB)), dim3(NT < 256 ? 256 : NT), 0, st>>>(a);
+    constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value, RPB = NT < 256 ? 256 / NT : 1, THREADS = NT < 256 ? 256 : NT;
+    for (int64_t left = a.rows; left > 0 && e == hipSuccess;) {
+      const int64_t n = std::min(left, most_groups(THREADS) * RPB), at = n * a.D;
+      a.rows = n;
+      rmsnorm_kernel<S, A, Y, V, NT, NC><<<dim3(static_cast<unsigned>((n + RPB - 1) / RPB)), dim3(THREADS), 0, st>>>(a);
+      e = hipGetLastError();
+      a.x = past(a.x, at * sizeof(S)); a.sum = past(a.sum, at * sizeof(S)); a.delta = past(a.delta, at * sizeof(A));
+      a.y = past(a.y, at * sizeof(Y)); a.y_scale = past(a.y_scale, n * sizeof(float));
+      left -= n;
+    }
   });
-  return hipGetLastError();
+  return e;
 }
 // whole pieces of 16 bytes of the stream where rows are made of them and start on them, else element by element
 template <class S, class A, class Y>

@@ -7,6 +7,7 @@
 // 64 bits (at position 10^6 a 32-bit product of position and frequency is off by 0.06 radians), reduced to a fraction of a turn there, and
 // its sine and cosine are taken in 32.  A thread takes one 16-byte piece of a head (two where the pairs are halves) at the same
 // place in several heads of a token, so that an angle serves them all.
+#include <algorithm>
 #include <cmath>
 
 #include "rows_common.h"
@@ -19,6 +20,7 @@ struct RotaryArgs {
   const int32_t *positions;      // [axes, period]
   const double *freq;            // [rot / 2]
   int64_t tokens, x_stride, out_stride, period;      // strides: elements from token to token
+  int64_t first;                 // number of the first token
   int heads, dh, rot, axes;
   int pieces, lanes;             // of a head: threads over it; threads over the heads
   int copy;                      // write the features behind `rot` too
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   if (slot >= tpb || token >= a.tokens) return;
   const int within = threadIdx.x % per_token;
   const int turning = a.rot / 2 / NP;
-  const int64_t at = token % a.period;
+  const int64_t at = (a.first + token) % a.period;
   const T *x = static_cast<const T *>(a.x) + token * a.x_stride;
   T *o = static_cast<T *>(a.out) + token * a.out_stride;
   for (int u = within; u < per_token; u += 256) {      // more than one round only where a head has more than 256 pieces
@@ -108,10 +110,17 @@ static hipError_t launch_rotary_v(RotaryArgs a, hipStream_t st) {
   a.lanes = lanes < a.heads ? lanes : a.heads;
   if (a.lanes > most) a.lanes = most;
   const int per_token = a.pieces * a.lanes, tpb = per_token < 256 ? 256 / per_token : 1;
-  const int64_t blocks = (a.tokens + tpb - 1) / tpb;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  rotary_kernel<T, V, HALVES><<<dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st>>>(a);
-  return hipGetLastError();
+  for (int64_t left = a.tokens; left > 0;) {
+    a.tokens = std::min(left, most_groups(256) * tpb);
+    rotary_kernel<T, V, HALVES><<<dim3(static_cast<unsigned>((a.tokens + tpb - 1) / tpb)), dim3(256), 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.x = static_cast<const T *>(a.x) + a.tokens * a.x_stride;
+    a.out = static_cast<T *>(a.out) + a.tokens * a.out_stride;
+    a.first += a.tokens;
+    left -= a.tokens;
+  }
+  return hipSuccess;
 }
 
 // The widest pieces, up to 16 bytes, that start on their own size in every head and that neither the turning part (either half of it where
@@ -142,7 +151,7 @@ static int rotary_impl(const char *fn, const void *x, void *out, const int32_t *
     return refuse(RESLIM_EINVAL, fn, "interleaved bf16 pairs must start on 4 bytes");
   if (tokens > 0 && x == out && x_stride != out_stride) return refuse(RESLIM_EINVAL, fn, "in place the strides must be the same");
   if (tokens == 0) return RESLIM_OK;
-  RotaryArgs a = {x, out, positions, freq, tokens, x_stride, out_stride, period, heads, dh, rot, axes, 0, 0, x != out, amplitude, sign};
+  RotaryArgs a = {x, out, positions, freq, tokens, x_stride, out_stride, period, 0, heads, dh, rot, axes, 0, 0, x != out, amplitude, sign};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const bool halves = layout == RESLIM_ROTARY_HALVES;
   const hipError_t e = dtype == RESLIM_BF16 ? (halves ? launch_rotary<bf16_t, true, 8>(a, st) : launch_rotary<bf16_t, false, 8>(a, st))

@@ -175,6 +175,9 @@ inline int refuse(int code, const char *fn, const char *why) noexcept {
 }
 inline int refuse_hip(const char *fn, hipError_t e) noexcept { return refuse(RESLIM_EHIP, fn, hipGetErrorString(e)); }
 
+// Work-groups of one launch: a launch holds fewer than 2^32 threads.
+constexpr int64_t most_groups(int threads) { return (int64_t{1} << 31) / threads; }
+
 inline bool aligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline size_t type_bytes(int dtype) { return dtype == RESLIM_F32 ? 4 : dtype == RESLIM_BF16 ? 2 : 1; }
 

@@ -191,6 +191,14 @@ def test_rows_behind_two_to_the_31_elements():
         assert P.worst(dx[at], want, bound * 1.01 + P.half(H) * want.abs() + 1e-40) <= 1
 
 
+def test_more_rows_than_a_launch_has_threads():
+    n = 68_000_000                                   # a wave each: 4.35e9 threads
+    x, y, scale = torch.ones(n, 64, dtype=H, device="cuda"), torch.zeros(n, 64, dtype=Q, device="cuda"), torch.zeros(n, device="cuda")
+    B.reslim_rmsnorm_fwd(x, torch.ones(64, device="cuda"), y, eps=0.0, y_scale=scale)
+    torch.cuda.synchronize()
+    assert bool((y.view(torch.uint8).view(-1, 4096)[::17] == 0x7E).all()) and bool((scale == scale[0]).all()) and abs(float(scale[0]) * 448 - 1) <= 4 * P.E
+
+
 def test_another_stream_and_a_captured_graph():
     x, delta, gamma = _inputs(300, 1024, F, H)
     st = torch.cuda.Stream()

@@ -125,6 +125,19 @@ def test_tokens_behind_two_to_the_31_elements():
         _check(was, x[at], pos[:, t].contiguous(), freq, heads, "half", 1.0)
 
 
+def test_more_tokens_than_a_launch_has_threads():
+    tokens, dh = 67_200_000, 62                      # 31 threads each, eight tokens to a work-group: a second launch from 2^26 on
+    x = torch.empty(tokens, 1, dh, dtype=H, device="cuda").normal_()
+    freq, _ = _table(62, 1)
+    pos = _positions(1, 1001)
+    sample = [slice(0, 2), slice(2 ** 26 - 2, 2 ** 26 + 2), slice(tokens - 2, tokens)]
+    kept = [x[at].clone() for at in sample]
+    B.reslim_rotary_fwd(x, x, pos, freq, heads=1, layout="half")
+    for at, was in zip(sample, kept):
+        t = torch.arange(at.start, at.stop, device="cuda") % 1001
+        _check(was, x[at], pos[:, t].contiguous(), freq, 1, "half", 1.0)
+
+
 def test_no_tokens():
     x = torch.empty(0, 4, 64, dtype=H, device="cuda")
     B.reslim_rotary_fwd(x, x, torch.empty(1, 0, dtype=torch.int32, device="cuda"), _table(64, 1)[0], heads=4)
