@@ -23,40 +23,58 @@ struct F32Args {
   int64_t a_step, b_step;              // elements from row to row (k contiguous) or from k to k (rows contiguous)
   int k_per;                           // k of a slice, a multiple of 16
   int64_t slice;                       // floats between the slices' results
+  float *sums;                         // kPlain with A read across: sums over k of A's rows [slices, M], or null
 };
 
 constexpr int kTile = 64, kBK = 32;
 constexpr int kPitchK = 36, kPitchRow = 68;      // floats of a [row][k] row and of a [k][row] one: 16-byte accesses of neighbouring rows fall into different banks
 
-// one operand's slab of 64 x 32 values from row `row0`, k `k0` on, eight of them a thread.  row_of: the operand's row for a row of the tile, or -1
+// one operand's slabs of 64 x 32 values, eight of them a thread.  row_of: the operand's row for a row of the tile, or -1; step: elements from
+// row to row (ALONG_K) or from k to k
 template <bool ALONG_K>
 struct Slab {
   static constexpr int kFloats = ALONG_K ? kTile * kPitchK : kBK * kPitchRow;
   float v[8];
+  const float *at;             // this thread's first value of slab 0
+  int64_t step;
+  int k, rows;                 // its k in a slab; ALONG_K: whether its row exists; else how many of its eight rows do
+  bool vec;
   template <class RowOf>
-  __device__ __forceinline__ void load(const float *p, int64_t step, bool vec, int k0, int k_end, RowOf &&row_of) {
+  __device__ __forceinline__ void start(const float *p, int64_t step_, RowOf &&row_of) {
     const int t = threadIdx.x;
+    step = step_;
+    vec = step % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
     if constexpr (ALONG_K) {                 // four threads to a row, eight consecutive k each
-      const int row = row_of(t / 4), k = k0 + t % 4 * 8;
-      const float *q = p + static_cast<int64_t>(row < 0 ? 0 : row) * step;
-      if (vec && row >= 0 && k + 8 <= k_end) {
-        fetch8(q + k);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = row >= 0 && k + i < k_end ? q[k + i] : 0.f;
-      }
+      const int row = row_of(t / 4);
+      k = t % 4 * 8;
+      rows = row >= 0;
+      at = p + static_cast<int64_t>(rows ? row : 0) * step + k;
     } else {                                 // eight threads to a k, eight consecutive rows each
-      const int k = k0 + t / 8, first = t % 8 * 8;
-      const int r0 = row_of(first), r1 = row_of(first + 7);
-      const float *q = p + static_cast<int64_t>(k < k_end ? k : k0) * step;
-      if (vec && k < k_end && r0 >= 0 && r1 == r0 + 7) {
-        fetch8(q + r0);
+      const int first = t % 8 * 8, row = row_of(first);
+      k = t / 8;
+      rows = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rows += row_of(first + i) >= 0;
+      vec = vec && rows == 8;
+      at = p + static_cast<int64_t>(k) * step + (rows ? row : 0);
+    }
+  }
+  __device__ __forceinline__ void load(int k0, int k_end) {
+    if constexpr (ALONG_K) {
+      const float *q = at + k0;
+      if (vec && rows && k0 + k + 8 <= k_end) {
+        fetch8(q);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = row_of(first + i);
-          v[i] = k < k_end && r >= 0 ? q[r] : 0.f;
-        }
+        for (int i = 0; i < 8; ++i) v[i] = rows && k0 + k + i < k_end ? q[i] : 0.f;
+      }
+    } else {
+      const float *q = at + k0 * step;
+      if (vec && k0 + k < k_end) {
+        fetch8(q);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k0 + k < k_end && i < rows ? q[i] : 0.f;
       }
     }
   }
@@ -100,22 +118,35 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
     }
   };
   static_assert(KIND != kGate || B_ALONG, "a gated tile's rows are not in a run");
-  const bool a_vec = g.a_step % 4 == 0 && (reinterpret_cast<uintptr_t>(g.a) & 15) == 0;
-  const bool b_vec = g.b_step % 4 == 0 && (reinterpret_cast<uintptr_t>(g.b) & 15) == 0;
   Slab<A_ALONG> sa;
   Slab<B_ALONG> sb;
   f32x16 acc = {};
-  sa.load(g.a, g.a_step, a_vec, k_begin, k_end, a_row);
-  sb.load(g.b, g.b_step, b_vec, k_begin, k_end, b_row);
+  // sums over k of A's rows, in the work-groups of the first column tile, from the registers that the slabs pass through
+  constexpr bool kSums = KIND == kPlain && !A_ALONG;
+  const bool sums = kSums && g.sums && blockIdx.x == 0;
+  float rs[kSums ? 8 : 1] = {};
+  auto add = [&]() {
+    if constexpr (kSums) {
+      if (sums) {                            // uniform
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rs[i] += sa.v[i];
+      }
+    }
+  };
+  sa.start(g.a, g.a_step, a_row);
+  sb.start(g.b, g.b_step, b_row);
+  sa.load(k_begin, k_end);
+  sb.load(k_begin, k_end);
   sa.store(As[0]);
   sb.store(Bs[0]);
+  add();
   __syncthreads();
   int buf = 0;
   for (int k0 = k_begin; k0 < k_end; k0 += kBK, buf ^= 1) {
     const bool more = k0 + kBK < k_end;
     if (more) {
-      sa.load(g.a, g.a_step, a_vec, k0 + kBK, k_end, a_row);
-      sb.load(g.b, g.b_step, b_vec, k0 + kBK, k_end, b_row);
+      sa.load(k0 + kBK, k_end);
+      sb.load(k0 + kBK, k_end);
     }
 #pragma unroll
     for (int s = 0; s < kBK / 8; ++s) {
@@ -128,8 +159,24 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
     if (more) {                              // the other buffer was last read before the barrier that ended the slab before
       sa.store(As[buf ^ 1]);
       sb.store(Bs[buf ^ 1]);
+      add();
     }
     __syncthreads();
+  }
+  if constexpr (kSums) {
+    if (sums) {                              // the 32 threads that share eight rows, in their order
+      float *part = As[0];                   // [32][64]
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part[threadIdx.x / 8 * kTile + threadIdx.x % 8 * 8 + i] = rs[i];
+      __syncthreads();
+      const int r = m0 + static_cast<int>(threadIdx.x);
+      if (threadIdx.x < kTile && r < g.M) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) s += part[i * kTile + threadIdx.x];
+        g.sums[static_cast<int64_t>(blockIdx.z) * g.M + r] = s;
+      }
+    }
   }
   // register r of the block: row 8 (r / 4) + 4 hi + r % 4, column l32: a store writes runs of 32 columns of two rows
   const int row0 = m0 + wm * 32 + 4 * hi;
@@ -172,22 +219,6 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
   }
 }
 
-// column sums of a [rows, N] matrix, a slab of rows for each work-group of 64 columns: partial [slabs, N]
-constexpr int kSumRows = 64;
-__global__ __launch_bounds__(256) void gated_colsum_kernel(const float *__restrict__ a, float *__restrict__ partial, int64_t rows, int N) {
-  __shared__ float sm[4][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), grp = threadIdx.x >> 6;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kSumRows, r1 = min(rows, r0 + kSumRows);
-  float s = 0.f;
-  if (c < N) {
-#pragma unroll 8
-    for (int64_t r = r0 + grp; r < r1; r += 4) s += a[r * N + c];
-  }
-  sm[grp][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (grp == 0 && c < N) partial[static_cast<int64_t>(blockIdx.y) * N + c] = (sm[0][threadIdx.x] + sm[1][threadIdx.x]) + (sm[2][threadIdx.x] + sm[3][threadIdx.x]);
-}
-
 template <F32Kind KIND, bool GELU, bool A_ALONG, bool B_ALONG>
 hipError_t launch(const F32Args &g, int slices, hipStream_t st) {
   constexpr int BNO = KIND == kGate ? kTile / 2 : kTile;
@@ -208,25 +239,28 @@ int f32_slices(int M, int N, int K) {
   const int64_t tiles = (static_cast<int64_t>(M) + kTile - 1) / kTile * ((static_cast<int64_t>(N) + kTile - 1) / kTile);
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, K / (8 * kBK))));
 }
-size_t slice_bytes(int M, int N, int K) {
+size_t slice_bytes(int M, int N, int K, int more) {      // more: floats of a slice beside the product
   const int s = f32_slices(M, N, K);
-  return s > 1 ? align256(static_cast<size_t>(s) * M * N * sizeof(float)) : 0;
+  return s > 1 ? align256(static_cast<size_t>(s) * (static_cast<size_t>(M) * N + more) * sizeof(float)) : 0;
 }
-// C = A B^T (+ bias), in slices where that pays
+// C = A B^T (+ bias; with g.sums set also the sums of A's rows), in slices where that pays
 template <bool A_ALONG, bool B_ALONG>
 hipError_t product(F32Args g, float *part, hipStream_t st) {
   int s = f32_slices(g.M, g.N, g.K);
   g.k_per = ((g.K + s - 1) / s + kBK - 1) / kBK * kBK;
   s = (g.K + g.k_per - 1) / g.k_per;
-  float *out = g.out;
+  float *out = g.out, *sums = g.sums;
+  const int64_t n = static_cast<int64_t>(g.M) * g.N;
   if (s > 1) {
     g.out = part;
-    g.slice = static_cast<int64_t>(g.M) * g.N;
+    g.sums = sums ? part + s * n : nullptr;
+    g.slice = n;
   }
-  const hipError_t e = launch<kPlain, false, A_ALONG, B_ALONG>(g, s, st);
-  return e == hipSuccess && s > 1 ? launch_partial_reduce(part, out, s, g.slice, g.slice, st) : e;
+  hipError_t e = launch<kPlain, false, A_ALONG, B_ALONG>(g, s, st);
+  if (e != hipSuccess || s == 1) return e;
+  e = launch_partial_reduce(part, out, s, n, n, st);
+  return e == hipSuccess && sums ? launch_partial_reduce(g.sums, sums, s, g.M, g.M, st) : e;
 }
-int sum_slabs(int M) { return (M + kSumRows - 1) / kSumRows; }
 
 // ------------------------------------------------------------------ few rows
 // A work-group owns 16 features of the result (with gate and up rows 32 rows of W) and all of K, its eight waves a run of K each, so that every
@@ -328,7 +362,7 @@ hipError_t launch_gated_f32_in(const GatedIn &in, bool gelu, hipStream_t st) {
   g.keep = static_cast<float *>(in.gu);
   return gelu ? launch<kGate, true, true, true>(g, 1, st) : launch<kGate, false, true, true>(g, 1, st);
 }
-size_t gated_f32_product_bytes(int M, int N, int K) { return slice_bytes(M, N, K); }
+size_t gated_f32_product_bytes(int M, int N, int K) { return slice_bytes(M, N, K, 0); }
 hipError_t launch_gated_f32_out(const float *h, const float *w_out, const float *b_out, float *y, int M, int D, int R, float *part, hipStream_t st) {
   if (few_rows(h, w_out, M, R)) {
     const FewArgs a = {h, w_out, b_out, y, nullptr, M, D, R};
@@ -347,18 +381,11 @@ hipError_t launch_gated_f32_dgate(const float *dy, const float *w_out, const flo
 hipError_t launch_gated_f32_dx(const float *d_gu, const float *w_in, float *dx, int M, int D, int R, float *part, hipStream_t st) {
   return product<true, false>(whole(d_gu, 2 * static_cast<int64_t>(R), w_in, D, dx, M, D, 2 * R), part, st);
 }
-size_t gated_f32_wgrad_bytes(int M, int N, int K) {
-  return std::max(slice_bytes(N, K, M), align256(static_cast<size_t>(sum_slabs(M)) * N * sizeof(float)));
-}
+size_t gated_f32_wgrad_bytes(int M, int N, int K) { return slice_bytes(N, K, M, N); }
 hipError_t launch_gated_f32_wgrad(const float *dy, const float *x, float *dw, float *db, int M, int N, int K, void *ws, hipStream_t st) {
-  float *part = static_cast<float *>(ws);
-  hipError_t e = product<false, false>(whole(dy, N, x, K, dw, N, K, M), part, st);
-  if (e != hipSuccess || !db) return e;
-  const int slabs = sum_slabs(M);
-  if (slabs > 65535) return hipErrorInvalidValue;
-  gated_colsum_kernel<<<dim3((N + 63) / 64, slabs), dim3(256), 0, st>>>(dy, part, M, N);
-  e = hipGetLastError();
-  return e == hipSuccess ? launch_partial_reduce(part, db, slabs, N, N, st) : e;
+  F32Args g = whole(dy, N, x, K, dw, N, K, M);
+  g.sums = db;
+  return product<false, false>(g, static_cast<float *>(ws), st);
 }
 
 }  // namespace reslim
