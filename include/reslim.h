@@ -586,7 +586,7 @@ int reslim_asc_forward(reslim_ctx *ctx, const reslim_asc_plan *plan, const float
  *   y       y_dtype [rows, D]: act_dtype, or RESLIM_E4M3 with y_scale float [rows]: row i stands for y[i, :] * y_scale[i],
  *           y_scale = max |.| of the row / 448 (a row of zeros has scale 0)
  * (stream_dtype, act_dtype) = (F32, F32), (F32, BF16) or (BF16, BF16); 1 <= D <= 16384; eps >= 0.  s is normalised before it
- * is rounded to the stream's type.  A value that is not finite stays in its row.  Buffers are aligned to their elements;
+ * is rounded to the stream's type.  mean(s^2) is an fp32 sum: |s| beyond 1e17 may overflow it, and y is then 0.  A value that is not finite stays in its row.  Buffers are aligned to their elements;
  * rows of a multiple of 16 bytes of the stream that start on 16 bytes run at full speed, others element by element. */
 int reslim_rmsnorm_fwd(const void *x, const void *delta, const float *gamma, float eps, int64_t rows, int32_t D,
                        int32_t stream_dtype, int32_t act_dtype, int32_t y_dtype, void *sum, void *y, float *y_scale,
@@ -645,8 +645,8 @@ int reslim_rotary_frequencies(int32_t rot, int32_t axes, double base, int32_t sc
  *   w_in  x_dtype [2R, D], gate rows then up rows; with RESLIM_E4M3 row n stands for w_in[n, :] * in_scale[n], in_scale float [2R]
  *   w_out act [D, R];  b_in float [2R], b_out float [D], either may be NULL
  * Types: x_dtype F32 (act float), BF16 (act bfloat16) or E4M3 (act bfloat16; forward only): x rows with x_scale float [rows] as
- * reslim_rmsnorm_fwd writes them.  D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
- * sizes, rows <= 4,000,000.  BF16 and E4M3 buffers start on 16 bytes. */
+ * reslim_rmsnorm_fwd writes them.  rows <= 2,000,000,000, D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
+ * sizes, rows <= 4,000,000 and at most 2^23 tiles of 64 rows by 32 of R, or 64 of D.  BF16 and E4M3 buffers start on 16 bytes. */
 enum { RESLIM_GATE_SILU = 0, RESLIM_GATE_GELU = 1 };
 typedef struct {
   const void *w_in;

@@ -1,8 +1,9 @@
 // Entry points of the gated feed-forward layer: checks, workspace, and the order of the launches.
 //
-// Forward: one launch for both projections, activation and product, one for the output map.  Gradient (bf16): transposed
-// copies of both matrices (the input gradients contract over the weights' rows), the hidden layer's gradient with the
-// gradients of gate and up in its epilogue, dx, and one launch for both weight gradients with their biases.
+// Forward: one launch for both projections, activation and product, one for the output map (two where its sum is sliced).  Gradient
+// (bf16): transposed copies of the matrices whose product does not run on 64 x 64 tiles (the input gradients contract over
+// the weights' rows, which those tiles alone read as they lie), the hidden layer's gradient with the gradients of gate and up in its
+// epilogue, dx, and one launch for both weight gradients with their biases.
 #include <algorithm>
 #include <mutex>
 
@@ -76,7 +77,7 @@ static void gated_ops(WgradOp (&op)[2], const void *d_gu, const void *x, const v
   op[0] = {d_gu, x, nullptr, nullptr, 2 * R, D};
   op[1] = {dy, h, nullptr, nullptr, D, R};
 }
-static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, int grad_dtype, void *base) {
+static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, void *base) {
   unsigned char *p = static_cast<unsigned char *>(base);
   size_t off = 0;
   auto take = [&](size_t bytes) { unsigned char *q = p + off; off += align256(bytes); return q; };
@@ -105,8 +106,12 @@ static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, int grad_dtype,
 // ------------------------------------------------------------------ checks
 static int gated_shape(const char *fn, int rows, int D, int R, int x_dtype) {
   if (x_dtype != RESLIM_F32 && x_dtype != RESLIM_BF16 && x_dtype != RESLIM_E4M3) return refuse(RESLIM_EINVAL, fn, "x_dtype must be RESLIM_F32, RESLIM_BF16 or RESLIM_E4M3");
-  if (rows < 0 || D < 1 || D > kGatedMaxD || R < 1 || R > kGatedMaxR) return refuse(RESLIM_ESHAPE, fn, "need rows >= 0, 1 <= D <= 16384 and 1 <= R <= 65536");
+  if (rows < 0 || rows > 2000000000 || D < 1 || D > kGatedMaxD || R < 1 || R > kGatedMaxR) return refuse(RESLIM_ESHAPE, fn, "need 0 <= rows <= 2,000,000,000, 1 <= D <= 16384 and 1 <= R <= 65536");
   if (x_dtype == RESLIM_F32 && rows > 4000000) return refuse(RESLIM_ESHAPE, fn, "the fp32 path takes up to 4,000,000 rows");
+  // ... and as many tiles of its widest layer and of its result as one launch has work-groups
+  const int64_t strips = (static_cast<int64_t>(rows) + 63) / 64;
+  if (x_dtype == RESLIM_F32 && strips * std::max((R + 31) / 32, (D + 63) / 64) > most_groups(256))
+    return refuse(RESLIM_ESHAPE, fn, "the fp32 path takes up to 2^23 tiles of 64 rows by 32 hidden or 64 output features");
   if (x_dtype == RESLIM_BF16 && (D % 64 || R % 64)) return refuse(RESLIM_ESHAPE, fn, "bf16 needs D and R to be multiples of 64");
   if (x_dtype == RESLIM_E4M3 && (D % 128 || R % 64)) return refuse(RESLIM_ESHAPE, fn, "e4m3 needs D to be a multiple of 128 and R of 64");
   return RESLIM_OK;
@@ -201,7 +206,7 @@ extern "C" int reslim_gated_mlp_bwd_workspace_bytes(int32_t rows, int32_t D, int
   if (rc != RESLIM_OK) return rc;
   const float *zeros = nullptr;
   if (x_dtype == RESLIM_BF16) (void)gated_ready(&zeros);      // the slices go by the device's compute units
-  *out = plan_gated_bwd(rows, D, R, x_dtype, grad_dtype, nullptr).total;
+  *out = plan_gated_bwd(rows, D, R, x_dtype, nullptr).total;
   return RESLIM_OK;
 }
 
@@ -225,7 +230,7 @@ extern "C" int reslim_gated_mlp_bwd(const void *x, const void *gu, const void *h
     e = hipGetLastError();
     return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
   }
-  const GatedBwdWs ws = plan_gated_bwd(rows, D, R, x_dtype, grad_dtype, workspace);
+  const GatedBwdWs ws = plan_gated_bwd(rows, D, R, x_dtype, workspace);
   if ((rc = gated_room(fn, workspace, ws_bytes, ws.total)) != RESLIM_OK) return rc;
   const bool gelu = gate == RESLIM_GATE_GELU;
   if (x_dtype == RESLIM_F32) {

@@ -12,6 +12,8 @@ struct GatedChoice {
   double us;
 };
 
+constexpr double kMostTiles = 1 << 23;      // work-groups of 256 threads that one launch takes; the persistent kernels need one for every compute unit
+
 // The smallest of the estimates of gemm_times and of those for the 64 x 64 tiles, in microseconds beside what every launch costs.  A slab of these takes
 // a work-group 0.26 us, its latency over the three in flight, while two lie on a compute unit, and a compute unit 0.27, what it draws
 // from L2 for one.  Slices of k make more work-groups of shorter sums, at the price of a second launch and of partial sums that are read
@@ -29,10 +31,11 @@ inline GatedChoice gated_choose(int M, int N, int cols, int slabs, GemmEpi epi, 
     if (us < best.us) best = {kernel, slices, us};
   };
   offer(kGemm128x256, 1, (count(128, 256) <= cus ? std::max(g.pp1, slabs * 0.8) : g.pp1) + other);
-  if (!e4m3) offer(kGemm128, 1, g.small + other);
+  if (!e4m3 && mid <= kMostTiles) offer(kGemm128, 1, g.small + other);
   for (int s = 1; s <= 32 && (s == 1 || slabs / s >= 4); ++s) {
     if (s > 1 && !sliceable) break;
     const int per = (slabs + s - 1) / s, n = (slabs + per - 1) / per;
+    if (tiles * n > kMostTiles) break;
     const double rounds = std::ceil(tiles * n / (2.0 * cus)), add = n > 1 ? 2.4 + 5e-6 / 4.5 * n * M * static_cast<double>(cols) : 0.0;
     offer(kGatedRing, n, 0.5 + std::max(rounds * per * 0.26, tiles * n * per * 0.27 / cus) + rounds * ring_epi[epi] + add);
     if (s > 1 && mid * n <= 3.0 * cus) {                   // 128 x 128 tiles, up to three on a compute unit

@@ -55,7 +55,7 @@ enum GatedEpilogue {
   kEpiKeep = 2,
   kEpiE4m3 = 4,
   EPI_DGATE = 64,         // acc = gradient of the hidden layer: out(act) = gradients of [gate | up]; + 1: GELU
-  EPI_SLICE = 96          // out(f32) [slices, M, N] = the sum over a slice of k (gemm_small.inc alone)
+  EPI_SLICE = 96          // out(f32) [slices, M, N] = the sum over a slice of k (128 x 128 and 64 x 64 tiles)
 };
 constexpr bool epi_gated(int epi) { return epi >= EPI_GATED && epi < EPI_DGATE; }
 constexpr bool epi_dgate(int epi) { return epi >= EPI_DGATE && epi < EPI_SLICE; }

@@ -68,6 +68,14 @@ def test_the_gpu_tests_reach_every_kernel(choose):
     assert {(RING, False), (RING, True), (SMALL, True)} <= met["dx"] and {k for k, _ in met["dx"]} & {WIDE, TALL}, met["dx"]
 
 
+@pytest.mark.parametrize("M", [2 ** 30 // 3, 2 ** 30, 2_000_000_000])
+def test_a_product_that_no_launch_holds_in_tiles_is_persistent(choose, M):
+    for D in (64, 128, 1024):
+        for n, (kernel, slices) in _products(choose, M, D, 64).items():
+            side, columns = 64 if kernel == RING else 128, 2 * 64 if n.startswith("in") else D if n in ("out", "dx") else 64
+            assert kernel in (WIDE, TALL) or -(-M // side) * -(-columns // side) * slices <= 2 ** 23, (n, kernel)
+
+
 def test_a_plan_is_well_formed_at_any_size(choose):
     r = random.Random(1)
     for _ in range(3000):

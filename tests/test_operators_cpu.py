@@ -120,7 +120,8 @@ def _fwd(x=p, xs=None, w=None, gate=0, rows=4, D=128, R=192, dt=BF16, y=p, ws=p,
     (dict(x=None), EINVAL), (dict(y=None), EINVAL), (dict(w_in=None), EINVAL), (dict(w_out=None), EINVAL), (dict(gate=2), EINVAL), (dict(gate=-1), EINVAL), (dict(dt=3), EINVAL),
     (dict(rows=-1), ESHAPE), (dict(D=0), ESHAPE), (dict(R=0), ESHAPE), (dict(D=96), ESHAPE), (dict(R=100), ESHAPE), (dict(D=16448), ESHAPE), (dict(R=65600), ESHAPE),
     (dict(dt=E4M3, xs=p, scale=p, D=192), ESHAPE), (dict(dt=E4M3, xs=p), EINVAL), (dict(dt=E4M3, scale=p), EINVAL), (dict(xs=p), EINVAL), (dict(scale=p), EINVAL),
-    (dict(dt=F32, rows=4000001), ESHAPE), (dict(x=p + 8), EINVAL), (dict(w_in=p + 8), EINVAL), (dict(w_out=p + 2), EINVAL), (dict(b_in=p + 4), EINVAL), (dict(b_out=p + 8), EINVAL),
+    (dict(dt=F32, rows=4000001), ESHAPE), (dict(dt=F32, rows=3999999, R=9000), ESHAPE), (dict(dt=F32, rows=3999999, D=16000), ESHAPE), (dict(rows=2000000001), ESHAPE),
+    (dict(x=p + 8), EINVAL), (dict(w_in=p + 8), EINVAL), (dict(w_out=p + 2), EINVAL), (dict(b_in=p + 4), EINVAL), (dict(b_out=p + 8), EINVAL),
     (dict(y=p + 8), EINVAL), (dict(dt=F32, x=p + 2), EINVAL), (dict(ws=None), EWS), (dict(ws=p + 16), EWS), (dict(n=1), EWS)])
 def test_gated_refusals(kw, code):
     assert _fwd(**kw) == code
