@@ -14,6 +14,8 @@ namespace reslim {
 namespace {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;      // four floats from any float on, one load all the same
 
 enum F32Kind { kPlain, kGate, kDGate };
 struct F32Args {
@@ -29,64 +31,63 @@ struct F32Args {
 constexpr int kTile = 64, kBK = 32;
 constexpr int kPitchK = 36, kPitchRow = 68;      // floats of a [row][k] row and of a [k][row] one: 16-byte accesses of neighbouring rows fall into different banks
 
-// one operand's slabs of 64 x 32 values, eight of them a thread.  row_of: the operand's row for a row of the tile, or -1; step: elements from
-// row to row (ALONG_K) or from k to k
+// One operand's slabs of 64 x 32 values, eight of them a thread.  row_of: the operand's row for a row of the tile, or -1; step: elements from
+// row to row (ALONG_K) or from k to k.  Rows that do not exist are read as others that do: they reach only results that are not stored.  No
+// lane of a whole slab's loads takes a path of its own, so that they stay in flight over a slab's products: with a condition
+// on every piece the compiler waited for one operand before it asked for the other.
 template <bool ALONG_K>
 struct Slab {
   static constexpr int kFloats = ALONG_K ? kTile * kPitchK : kBK * kPitchRow;
-  float v[8];
-  const float *at;             // this thread's first value of slab 0
+  f32x4 v[2];
+  const float *at[2];          // this thread's first values of slab 0: ALONG_K four k of two rows, else four rows at two k
   int64_t step;
-  int k, rows;                 // its k in a slab; ALONG_K: whether its row exists; else how many of its eight rows do
-  bool vec;
+  int k, last;                 // its first k in a slab; not ALONG_K: the last of its four rows that exists
+  bool fours;                  // not ALONG_K: all or none of any thread's four rows exist
   template <class RowOf>
-  __device__ __forceinline__ void start(const float *p, int64_t step_, RowOf &&row_of) {
+  __device__ __forceinline__ void start(const float *p, int64_t step_, int rows, RowOf &&row_of) {
     const int t = threadIdx.x;
     step = step_;
-    vec = step % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
-    if constexpr (ALONG_K) {                 // four threads to a row, eight consecutive k each
-      const int row = row_of(t / 4);
-      k = t % 4 * 8;
-      rows = row >= 0;
-      at = p + static_cast<int64_t>(rows ? row : 0) * step + k;
-    } else {                                 // eight threads to a k, eight consecutive rows each
-      const int first = t % 8 * 8, row = row_of(first);
-      k = t / 8;
-      rows = 0;
+    if constexpr (ALONG_K) {                 // eight threads to a row
+      k = t % 8 * 4;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rows += row_of(first + i) >= 0;
-      vec = vec && rows == 8;
-      at = p + static_cast<int64_t>(k) * step + (rows ? row : 0);
+      for (int j = 0; j < 2; ++j) at[j] = p + static_cast<int64_t>(max(row_of(t / 8 + 32 * j), 0)) * step + k;
+    } else {                                 // sixteen threads to a k
+      const int first = t % 16 * 4;
+      k = t / 16;
+      last = 0;
+      fours = rows % 4 == 0 || row_of(kTile - 1) >= 0;
+#pragma unroll
+      for (int i = 1; i < 4; ++i) last += row_of(first + i) >= 0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) at[j] = p + static_cast<int64_t>(k + 16 * j) * step + max(row_of(first), 0);
     }
   }
   __device__ __forceinline__ void load(int k0, int k_end) {
-    if constexpr (ALONG_K) {
-      const float *q = at + k0;
-      if (vec && rows && k0 + k + 8 <= k_end) {
-        fetch8(q);
+    const float *q[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) q[j] = ALONG_K ? at[j] + k0 : at[j] + k0 * step;
+    if (k0 + kBK <= k_end) {                 // uniform
+      if (ALONG_K || fours) {               // uniform
+#pragma unroll
+        for (int j = 0; j < 2; ++j) v[j] = *reinterpret_cast<const f32x4_any *>(q[j]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = rows && k0 + k + i < k_end ? q[i] : 0.f;
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[j][i] = q[j][min(i, last)];
       }
     } else {
-      const float *q = at + k0 * step;
-      if (vec && k0 + k < k_end) {
-        fetch8(q);
-      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k0 + k < k_end && i < rows ? q[i] : 0.f;
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = k0 + k + (ALONG_K ? i : 16 * j) < k_end ? q[j][ALONG_K ? i : min(i, last)] : 0.f;
     }
-  }
-  __device__ __forceinline__ void fetch8(const float *q) {
-    const float4 a = *reinterpret_cast<const float4 *>(q), b = *reinterpret_cast<const float4 *>(q + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
   __device__ __forceinline__ void store(float *lds) const {
     const int t = threadIdx.x;
-    float *q = lds + (ALONG_K ? t / 4 * kPitchK + t % 4 * 8 : t / 8 * kPitchRow + t % 8 * 8);
-    *reinterpret_cast<float4 *>(q) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(q + 4) = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<f32x4 *>(lds + (ALONG_K ? (t / 8 + 32 * j) * kPitchK + t % 8 * 4 : (t / 16 + 16 * j) * kPitchRow + t % 16 * 4)) = v[j];
   }
   // four consecutive k of a row of the tile
   static __device__ __forceinline__ void read(const float *lds, int row, int k, float (&f)[4]) {
@@ -124,56 +125,70 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(F32Args g) {
   // sums over k of A's rows, in the work-groups of the first column tile, from the registers that the slabs pass through
   constexpr bool kSums = KIND == kPlain && !A_ALONG;
   const bool sums = kSums && g.sums && blockIdx.x == 0;
-  float rs[kSums ? 8 : 1] = {};
+  float rs[kSums ? 4 : 1] = {};
   auto add = [&]() {
     if constexpr (kSums) {
       if (sums) {                            // uniform
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rs[i] += sa.v[i];
+        for (int i = 0; i < 4; ++i) rs[i] += sa.v[0][i] + sa.v[1][i];
       }
     }
   };
-  sa.start(g.a, g.a_step, a_row);
-  sb.start(g.b, g.b_step, b_row);
+  sa.start(g.a, g.a_step, g.M, a_row);
+  sb.start(g.b, g.b_step, g.N, b_row);
   sa.load(k_begin, k_end);
   sb.load(k_begin, k_end);
   sa.store(As[0]);
   sb.store(Bs[0]);
   add();
+  if (k_begin + kBK < k_end) {
+    sa.load(k_begin + kBK, k_end);
+    sb.load(k_begin + kBK, k_end);
+  }
   __syncthreads();
+  // A slab's turn begins with its first reads and with the next slab's way from registers to the other buffer (last read before the barrier
+  // that ended the slab before), so that nothing but the barrier stands between the products of two slabs.
   int buf = 0;
   for (int k0 = k_begin; k0 < k_end; k0 += kBK, buf ^= 1) {
-    const bool more = k0 + kBK < k_end;
-    if (more) {
-      sa.load(k0 + kBK, k_end);
-      sb.load(k0 + kBK, k_end);
-    }
+    float x[kBK / 8][4], w[kBK / 8][4];
+    auto read = [&](int s) {
+      Slab<A_ALONG>::read(As[buf], wm * 32 + l32, 8 * s + 4 * hi, x[s]);
+      Slab<B_ALONG>::read(Bs[buf], wn * 32 + l32, 8 * s + 4 * hi, w[s]);
+    };
+    auto multiply = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < kBK / 8; ++s) {
-      float x[4], w[4];
-      Slab<A_ALONG>::read(As[buf], wm * 32 + l32, 8 * s + 4 * hi, x);
-      Slab<B_ALONG>::read(Bs[buf], wn * 32 + l32, 8 * s + 4 * hi, w);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], w[i], acc, 0, 0, 0);
-    }
-    if (more) {                              // the other buffer was last read before the barrier that ended the slab before
+      for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[s][i], w[s][i], acc, 0, 0, 0);
+    };
+    read(0);
+    read(1);
+    if (k0 + kBK < k_end) {
       sa.store(As[buf ^ 1]);
       sb.store(Bs[buf ^ 1]);
       add();
+      if (k0 + 2 * kBK < k_end) {
+        sa.load(k0 + 2 * kBK, k_end);
+        sb.load(k0 + 2 * kBK, k_end);
+      }
     }
+    multiply(0);
+    read(2);
+    read(3);
+    multiply(1);
+    multiply(2);
+    multiply(3);
     __syncthreads();
   }
   if constexpr (kSums) {
-    if (sums) {                              // the 32 threads that share eight rows, in their order
-      float *part = As[0];                   // [32][64]
+    if (sums) {                              // the 16 threads that share four rows, in their order
+      float *part = As[0];                   // [16][64]
 #pragma unroll
-      for (int i = 0; i < 8; ++i) part[threadIdx.x / 8 * kTile + threadIdx.x % 8 * 8 + i] = rs[i];
+      for (int i = 0; i < 4; ++i) part[threadIdx.x / 16 * kTile + threadIdx.x % 16 * 4 + i] = rs[i];
       __syncthreads();
       const int r = m0 + static_cast<int>(threadIdx.x);
       if (threadIdx.x < kTile && r < g.M) {
         float s = 0.f;
-#pragma unroll 8
-        for (int i = 0; i < 32; ++i) s += part[i * kTile + threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i * kTile + threadIdx.x];
         g.sums[static_cast<int64_t>(blockIdx.z) * g.M + r] = s;
       }
     }
@@ -234,6 +249,30 @@ F32Args whole(const float *a, int64_t a_step, const float *b, int64_t b_step, fl
   return g;
 }
 
+// out [n] and sums [m] (or null): the slices' values added in their order, four floats a thread
+__global__ __launch_bounds__(256) void gated_f32_sum_kernel(const float *__restrict__ part, float *__restrict__ out, int64_t n, float *__restrict__ sums, int64_t m, int slices) {
+  int64_t at = 4 * (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x);
+  if (at >= n) {                             // whole work-groups take the product, the ones behind them the sums
+    at -= (n + 1023) / 1024 * 1024;
+    if (at < 0 || at >= m) return;
+    part += slices * n;
+    out = sums;
+    n = m;
+  }
+  if (at + 4 <= n) {
+    f32x4 s = *reinterpret_cast<const f32x4_any *>(part + at);
+#pragma unroll 4
+    for (int k = 1; k < slices; ++k) s += *reinterpret_cast<const f32x4_any *>(part + k * n + at);
+    *reinterpret_cast<f32x4_any *>(out + at) = s;
+  } else {
+    for (; at < n; ++at) {
+      float s = part[at];
+      for (int k = 1; k < slices; ++k) s += part[k * n + at];
+      out[at] = s;
+    }
+  }
+}
+
 // Slices of k: as many as fill the four work-groups that a compute unit holds, of at least eight slabs each.
 int f32_slices(int M, int N, int K) {
   const int64_t tiles = (static_cast<int64_t>(M) + kTile - 1) / kTile * ((static_cast<int64_t>(N) + kTile - 1) / kTile);
@@ -256,10 +295,11 @@ hipError_t product(F32Args g, float *part, hipStream_t st) {
     g.sums = sums ? part + s * n : nullptr;
     g.slice = n;
   }
-  hipError_t e = launch<kPlain, false, A_ALONG, B_ALONG>(g, s, st);
+  const hipError_t e = launch<kPlain, false, A_ALONG, B_ALONG>(g, s, st);
   if (e != hipSuccess || s == 1) return e;
-  e = launch_partial_reduce(part, out, s, n, n, st);
-  return e == hipSuccess && sums ? launch_partial_reduce(g.sums, sums, s, g.M, g.M, st) : e;
+  const int64_t groups = (n + 1023) / 1024 + (sums ? (g.M + 1023) / 1024 : 0);
+  gated_f32_sum_kernel<<<dim3(static_cast<unsigned>(groups)), dim3(256), 0, st>>>(part, out, n, sums, sums ? g.M : 0, s);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ few rows
@@ -271,7 +311,6 @@ struct FewArgs {
   float *out, *keep;           // keep: gated, [gate | up] or null
   int M, N, K;                 // N: rows of one weight matrix
 };
-typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 template <int P, bool GELU>
 __global__ __launch_bounds__(512) void gated_f32_few_kernel(FewArgs a) {
