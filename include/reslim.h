@@ -586,8 +586,8 @@ int reslim_asc_forward(reslim_ctx *ctx, const reslim_asc_plan *plan, const float
  *   y       y_dtype [rows, D]: act_dtype, or RESLIM_E4M3 with y_scale float [rows]: row i stands for y[i, :] * y_scale[i],
  *           y_scale = max |.| of the row / 448 (a row of zeros has scale 0)
  * (stream_dtype, act_dtype) = (F32, F32), (F32, BF16) or (BF16, BF16); 1 <= D <= 16384; eps >= 0.  s is normalised before it
- * is rounded to the stream's type.  mean(s^2) is an fp32 sum: |s| beyond 1e17 may overflow it, and y is then 0.  A value that is not finite stays in its row.  Buffers are aligned to their elements;
- * rows of a multiple of 16 bytes of the stream that start on 16 bytes run at full speed, others element by element. */
+ * is rounded to the stream's type.  mean(s^2) is an fp32 sum: |s| beyond 1e17 may overflow it, and y is then 0.  A value that is not finite stays in its row.  Buffers are aligned to their elements.
+ * Rows of a multiple of 16 bytes of the stream are the fastest. */
 int reslim_rmsnorm_fwd(const void *x, const void *delta, const float *gamma, float eps, int64_t rows, int32_t D,
                        int32_t stream_dtype, int32_t act_dtype, int32_t y_dtype, void *sum, void *y, float *y_scale,
                        void *hip_stream);
@@ -617,8 +617,8 @@ int reslim_rmsnorm_bwd(const void *sum, const void *dy, const float *gamma, floa
  *             Only the `heads` rotated heads are written
  *   positions int32 [axes, period];  freq double [rot / 2];  dtype RESLIM_F32 or RESLIM_BF16
  * rot: a multiple of 2 * axes, at most dh; dh even, at most 1024; x_stride, out_stride >= heads * dh.  Interleaved bf16 pairs
- * start on 4 bytes.  Fastest where 16-byte pieces start in every head and neither rot (rot / 2 for pairs of halves) nor dh
- * ends inside one; otherwise pieces are as narrow as that takes.
+ * start on 4 bytes.  Fastest where neither rot (rot / 2 for pairs of halves) nor dh - rot ends inside 16 bytes; otherwise
+ * pieces are as narrow as that takes.
  * reslim_rotary_bwd is the gradient, the same turn backwards: d_out in, d_x out (in place allowed). */
 enum { RESLIM_ROTARY_INTERLEAVED = 0, RESLIM_ROTARY_HALVES = 1 };
 int reslim_rotary_fwd(const void *x, void *out, const int32_t *positions, const double *freq, int64_t tokens, int64_t x_stride,

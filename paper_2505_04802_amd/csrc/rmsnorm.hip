@@ -5,9 +5,10 @@
 //
 // Both move every element once and compute next to nothing, so memory bounds them: a row stays in the registers of the
 // threads that share it (a wave up to 1024 features, a work-group beyond) between the sums and the result, every load
-// of a row is issued before the first is used, and 16 bytes of the stream is what a thread takes at a time.  Sums are
-// fp32 in an order that depends on the row's width and alignment alone, so a row's result does not depend on the
-// others.  s is normalised before it is rounded to the stream's type.
+// of a row is issued before the first is used, and 16 bytes of the stream is what a thread takes at a time, wherever they start.  Sums are
+// fp32 in an order that depends on the row's width alone, so a row's result does not depend on the
+// others.  s is normalised before it is rounded to the stream's type.  161,408 x 1024 (fp32 stream, bf16 addend and result) take 356 us, 5.6 TB/s,
+// 37,520 x 4096 (bf16, e4m3 result) 187 us, 5.75 TB/s; a large copy reaches 4.9.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,7 +26,10 @@ struct NormArgs {
   int D;
 };
 
-template <class S, class A, class Y, int V, int NT, int NC>
+// TAIL: a row ends inside a piece.  Its loads reach into the next row, as far as there is one, so that they go out with the others; what
+// they bring from there is not used, and the piece is stored element by element.  At 29,304 x 4095 5.2 TB/s (fp32 stream, bf16 result) where
+// 4096 features run at 5.6; element by element throughout, 2.3.
+template <class S, class A, class Y, int V, int NT, int NC, bool TAIL>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;
   __shared__ float box[2][NT / 64];
@@ -35,13 +39,24 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
   const int64_t at = row * a.D;
   const S *x = static_cast<const S *>(a.x) + at;
   const A *d = static_cast<const A *>(a.delta) + at;
+  const int64_t most = TAIL ? a.rows * a.D - at : 0;       // elements from this row on
+  auto store = [&](auto *p, int k, const float (&from)[V]) {
+    typedef typename std::remove_reference<decltype(*p)>::type T;
+    if (!TAIL || k + V <= a.D) Piece<T, V>::store(p + k, from);
+    else store_some<T, V>(p + k, a.D - k, from);
+  };
   float v[NC][V], w[NC][V];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int k = (i * NT + t) * V;
     if (k < a.D) {
-      Piece<S, V>::load(x + k, v[i]);
-      if (a.delta) Piece<A, V>::load(d + k, w[i]);
+      if (!TAIL || k + V <= most) {
+        Piece<S, V>::load(x + k, v[i]);
+        if (a.delta) Piece<A, V>::load(d + k, w[i]);
+      } else {
+        load_some<S, V>(x + k, a.D - k, v[i]);
+        if (a.delta) load_some<A, V>(d + k, a.D - k, w[i]);
+      }
     }
   }
   float sq = 0.f;
@@ -52,9 +67,11 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
       if (a.delta) {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[i][j] += w[i][j];
-        if (a.sum) Piece<S, V>::store(static_cast<S *>(a.sum) + at + k, v[i]);
-      } else if (a.sum) {
-        Piece<S, V>::store(static_cast<S *>(a.sum) + at + k, v[i]);
+      }
+      if (a.sum) store(static_cast<S *>(a.sum) + at, k, v[i]);
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j] = k + j < a.D ? v[i][j] : 0.f;
       }
 #pragma unroll
       for (int j = 0; j < V; ++j) sq = fmaf(v[i][j], v[i][j], sq);
@@ -67,13 +84,14 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
     const int k = (i * NT + t) * V;
     if (k < a.D) {
       float g[V];
-      Piece<float, V>::load(a.gamma + k, g);
+      if (!TAIL || k + V <= a.D) Piece<float, V>::load(a.gamma + k, g);
+      else load_some<float, V>(a.gamma + k, a.D - k, g);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         v[i][j] = v[i][j] * r * g[j];
         top = fmaxf(top, fabsf(v[i][j]));
       }
-      if constexpr (!std::is_same<Y, e4m3_t>::value) Piece<Y, V>::store(static_cast<Y *>(a.y) + at + k, v[i]);
+      if constexpr (!std::is_same<Y, e4m3_t>::value) store(static_cast<Y *>(a.y) + at, k, v[i]);
     }
   }
   if constexpr (std::is_same<Y, e4m3_t>::value) {
@@ -87,7 +105,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
       if (k < a.D) {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[i][j] *= up;
-        Piece<e4m3_t, V>::store(static_cast<e4m3_t *>(a.y) + at + k, v[i]);
+        store(static_cast<e4m3_t *>(a.y) + at, k, v[i]);
       }
     }
   }
@@ -103,46 +121,53 @@ struct NormBwdArgs {
   int D;
 };
 
-// A work-group takes every gridDim-th row (four of them at widths of a wave), so that the chip works on neighbouring rows, and keeps its part of dgamma in registers.  The next row's loads are in flight while a row is summed and
-// written: without them 37,520 x 4096 (fp32 stream, bf16 gradient, skip gradient) took 592 us, 4.15 TB/s.
-template <class S, class A, int V, int NT, int NC>
+// A work-group takes every gridDim-th row (four of them at widths of a wave), so that the chip works on neighbouring rows, and keeps its part of
+// dgamma in registers.  The next row's loads are in flight while a row is summed and written: 37,520 x 4096 (fp32 stream, bf16 gradient, skip
+// gradient) 467 us, 5.27 TB/s; without them 592, 4.15 TB/s.
+template <class S, class A, int V, int NT, int NC, bool TAIL>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_bwd_kernel(NormBwdArgs a) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;
   __shared__ float box[2][2 * (NT / 64)];
   __shared__ float sm[RPB > 1 ? RPB : 1][RPB > 1 ? NT * NC * V : 1];
   const int t = threadIdx.x % NT, part = threadIdx.x / NT;
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * RPB + part, stride = static_cast<int64_t>(gridDim.x) * RPB;
-  // element by element the gains are read again where they are used: sixteen of them do not fit beside the rest
-  constexpr bool kKeep = V > 1;
-  float gam[kKeep ? NC : 1][V], acc[NC][V];
+  float gam[NC][V], acc[NC][V];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int k = (i * NT + t) * V;
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[i][j] = 0.f;
-    if constexpr (kKeep) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) gam[i][j] = 0.f;
-      if (k < a.D) Piece<float, V>::load(a.gamma + k, gam[i]);
+    for (int j = 0; j < V; ++j) gam[i][j] = acc[i][j] = 0.f;
+    if (k < a.D) {
+      if (!TAIL || k + V <= a.D) Piece<float, V>::load(a.gamma + k, gam[i]);
+      else load_some<float, V>(a.gamma + k, a.D - k, gam[i]);
     }
   }
-  auto gain = [&](int i, int j) { return kKeep ? gam[kKeep ? i : 0][j] : a.gamma[(i * NT + t) * V + j]; };
   const float inv_d = 1.0f / static_cast<float>(a.D);
-  // single elements, and sixteen to a thread in work-groups of sixteen waves, leave no registers for a second row
-  constexpr bool kAhead = V > 1 && (NT < 1024 || NC * V <= 8);
-  typedef typename std::conditional<kAhead, Held<S, V>, Loaded<S, V>>::type RowS;
-  typedef typename std::conditional<kAhead, Held<A, V>, Loaded<A, V>>::type RowA;
-  RowS s[NC], z[NC], sn[kAhead ? NC : 1], zn[kAhead ? NC : 1];
-  RowA e[NC], en[kAhead ? NC : 1];
+  // Sixteen elements to a thread in work-groups of sixteen waves leave no registers for a second row, nor for a tail that has to be told
+  // from the next row's elements: it is loaded element by element there, and the skip gradient with its tail where it is added.
+  constexpr bool kAhead = NT < 1024 || NC * V <= 8, kReach = TAIL && kAhead;
+  Held<S, V> s[NC], z[NC], sn[kAhead ? NC : 1], zn[kAhead ? NC : 1];
+  Held<A, V> e[NC], en[kAhead ? NC : 1];
+  auto store = [&](auto *p, int k, const float (&from)[V]) {
+    typedef typename std::remove_reference<decltype(*p)>::type T;
+    if (!TAIL || k + V <= a.D) Piece<T, V>::store(p + k, from);
+    else store_some<T, V>(p + k, a.D - k, from);
+  };
   auto load = [&](int64_t row, auto &ds, auto &de, auto &dz) {
     const int64_t at = row * a.D;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int k = (i * NT + t) * V;
       if (k < a.D) {
-        ds[i].load(static_cast<const S *>(a.s) + at + k);
-        de[i].load(static_cast<const A *>(a.dy) + at + k);
-        if (a.d_sum) dz[i].load(static_cast<const S *>(a.d_sum) + at + k);
+        if (!TAIL || (kReach ? at + k + V <= a.rows * a.D : k + V <= a.D)) {
+          ds[i].load(static_cast<const S *>(a.s) + at + k);
+          de[i].load(static_cast<const A *>(a.dy) + at + k);
+          if ((!TAIL || kReach) && a.d_sum) dz[i].load(static_cast<const S *>(a.d_sum) + at + k);
+        } else {
+          ds[i].load_some(static_cast<const S *>(a.s) + at + k, a.D - k);
+          de[i].load_some(static_cast<const A *>(a.dy) + at + k, a.D - k);
+          if (kReach && a.d_sum) dz[i].load_some(static_cast<const S *>(a.d_sum) + at + k, a.D - k);
+        }
       }
     }
   };
@@ -163,8 +188,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_bwd_kernel(NormBw
       if ((i * NT + t) * V < a.D) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          sq = fmaf(s[i][j], s[i][j], sq);
-          gs = fmaf(gain(i, j) * e[i][j], s[i][j], gs);
+          const bool in = !kReach || (i * NT + t) * V + j < a.D;
+          const float f = in ? s[i][j] : 0.f;
+          sq = fmaf(f, f, sq);
+          gs = fmaf(gam[i][j] * (in ? e[i][j] : 0.f), f, gs);
         }
       }
     row_sum2<NT>(sq, gs, box[turn]);
@@ -174,16 +201,21 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_bwd_kernel(NormBw
     for (int i = 0; i < NC; ++i) {
       const int k = (i * NT + t) * V;
       if (k < a.D) {
+        if constexpr (TAIL && !kReach) {
+          const S *from = static_cast<const S *>(a.d_sum) + at + k;
+          if (a.d_sum && k + V <= a.D) z[i].load(from);
+          else if (a.d_sum) z[i].load_some(from, a.D - k);
+        }
         float o[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float h = s[i][j] * r;
           acc[i][j] = fmaf(e[i][j], h, acc[i][j]);
-          o[j] = r * (gain(i, j) * e[i][j] - h * c);
+          o[j] = r * (gam[i][j] * e[i][j] - h * c);
           if (a.d_sum) o[j] += z[i][j];
         }
-        Piece<S, V>::store(static_cast<S *>(a.dx) + at + k, o);
-        if (a.d_delta) Piece<A, V>::store(static_cast<A *>(a.d_delta) + at + k, o);
+        store(static_cast<S *>(a.dx) + at, k, o);
+        if (a.d_delta) store(static_cast<A *>(a.d_delta) + at, k, o);
       }
     }
   }
@@ -204,7 +236,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_bwd_kernel(NormBw
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int k = (i * NT + t) * V;
-      if (k < a.D) Piece<float, V>::store(out + k, acc[i]);
+      if (k < a.D) store(out, k, acc[i]);
     }
   }
 }
@@ -228,12 +260,12 @@ static void norm_shape(int D, F &&f) {
   typedef integral_constant<int, 256> Four;
   typedef integral_constant<int, 1024> Sixteen;
   typedef integral_constant<int, 16 / V> Full;
-  typedef integral_constant<int, V == 1 ? 4 : 8 / V> Part;
+  typedef integral_constant<int, 8 / V> Part;
   (void)(fits(Wave{}, integral_constant<int, 1>{}) || fits(Wave{}, Part{}) || fits(Wave{}, Full{}) || fits(Four{}, Part{}) || fits(Four{}, Full{}) ||
          fits(Sixteen{}, Part{}) || fits(Sixteen{}, Full{}));
 }
 
-template <class S, class A, class Y, int V>
+template <class S, class A, class Y, int V, bool TAIL>
 static hipError_t launch_norm_v(NormArgs a, hipStream_t st) {
   auto past = [](auto *p, int64_t bytes) { return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + bytes) : p; };
   hipError_t e = hipSuccess;
@@ -242,7 +274,7 @@ static hipError_t launch_norm_v(NormArgs a, hipStream_t st) {
     for (int64_t left = a.rows; left > 0 && e == hipSuccess;) {
       const int64_t n = std::min(left, most_groups(THREADS) * RPB), at = n * a.D;
       a.rows = n;
-      rmsnorm_kernel<S, A, Y, V, NT, NC><<<dim3(static_cast<unsigned>((n + RPB - 1) / RPB)), dim3(THREADS), 0, st>>>(a);
+      rmsnorm_kernel<S, A, Y, V, NT, NC, TAIL><<<dim3(static_cast<unsigned>((n + RPB - 1) / RPB)), dim3(THREADS), 0, st>>>(a);
       e = hipGetLastError();
       a.x = past(a.x, at * sizeof(S)); a.sum = past(a.sum, at * sizeof(S)); a.delta = past(a.delta, at * sizeof(A));
       a.y = past(a.y, at * sizeof(Y)); a.y_scale = past(a.y_scale, n * sizeof(float));
@@ -251,15 +283,14 @@ static hipError_t launch_norm_v(NormArgs a, hipStream_t st) {
   });
   return e;
 }
-// whole pieces of 16 bytes of the stream where rows are made of them and start on them, else element by element
+// pieces of 16 bytes of the stream, from any address on
 template <class S, class A, class Y>
 static hipError_t launch_norm(const NormArgs &a, hipStream_t st) {
   constexpr int V = 16 / sizeof(S);
-  const bool whole = a.D % V == 0 && aligned(a.x, 16) && aligned(a.sum, 16) && aligned(a.delta, V * sizeof(A)) && aligned(a.y, V * sizeof(Y)) && aligned(a.gamma, 16);
-  return whole ? launch_norm_v<S, A, Y, V>(a, st) : launch_norm_v<S, A, Y, 1>(a, st);
+  return a.D % V ? launch_norm_v<S, A, Y, V, true>(a, st) : launch_norm_v<S, A, Y, V, false>(a, st);
 }
 
-template <class S, class A, int V>
+template <class S, class A, int V, bool TAIL>
 static hipError_t launch_norm_bwd_v(NormBwdArgs a, float *dgamma, hipStream_t st) {
   int64_t groups = 0;
   if (a.rows > 0) {
@@ -267,7 +298,7 @@ static hipError_t launch_norm_bwd_v(NormBwdArgs a, float *dgamma, hipStream_t st
       constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value, RPB = NT < 256 ? 256 / NT : 1;
       groups = norm_bwd_groups((a.rows + RPB - 1) / RPB);
       if (groups == 1) a.partial = dgamma;
-      rmsnorm_bwd_kernel<S, A, V, NT, NC><<<dim3(static_cast<unsigned>(groups)), dim3(NT < 256 ? 256 : NT), 0, st>>>(a);
+      rmsnorm_bwd_kernel<S, A, V, NT, NC, TAIL><<<dim3(static_cast<unsigned>(groups)), dim3(NT < 256 ? 256 : NT), 0, st>>>(a);
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || groups == 1) return e;
@@ -277,9 +308,7 @@ static hipError_t launch_norm_bwd_v(NormBwdArgs a, float *dgamma, hipStream_t st
 template <class S, class A>
 static hipError_t launch_norm_bwd(const NormBwdArgs &a, float *dgamma, hipStream_t st) {
   constexpr int V = 16 / sizeof(S);
-  const bool whole = a.D % V == 0 && aligned(a.s, 16) && aligned(a.d_sum, 16) && aligned(a.dx, 16) && aligned(a.dy, V * sizeof(A)) &&
-                     aligned(a.d_delta, V * sizeof(A)) && aligned(a.gamma, 16) && aligned(dgamma, 16);
-  return whole ? launch_norm_bwd_v<S, A, V>(a, dgamma, st) : launch_norm_bwd_v<S, A, 1>(a, dgamma, st);
+  return a.D % V ? launch_norm_bwd_v<S, A, V, true>(a, dgamma, st) : launch_norm_bwd_v<S, A, V, false>(a, dgamma, st);
 }
 
 static int norm_check(const char *fn, int64_t rows, int D, float eps, int stream_dtype, int act_dtype) {

@@ -123,13 +123,11 @@ static hipError_t launch_rotary_v(RotaryArgs a, hipStream_t st) {
   return hipSuccess;
 }
 
-// The widest pieces, up to 16 bytes, that start on their own size in every head and that neither the turning part (either half of it where
-// pairs are halves) nor the head ends inside.  With single elements 25,986 x 20 heads of 96, 24 of them turning as halves, took 117 us.
+// The widest pieces, up to 16 bytes, that neither the turning part (either half of it where pairs are halves) nor the head ends inside.  With single elements 25,986 x 20 heads of 96, 24 of them turning as halves, took 117 us.
 template <class T, bool HALVES, int V>
 static hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st) {
   if constexpr (V > (HALVES ? 1 : 2)) {
-    const bool starts = aligned(a.x, V * sizeof(T)) && aligned(a.out, V * sizeof(T)) && a.dh % V == 0 && a.x_stride % V == 0 && a.out_stride % V == 0;
-    if (!starts || a.rot % (HALVES ? 2 * V : V)) return launch_rotary<T, HALVES, V / 2>(a, st);
+    if ((a.dh - a.rot) % V || a.rot % (HALVES ? 2 * V : V)) return launch_rotary<T, HALVES, V / 2>(a, st);
   }
   return launch_rotary_v<T, V, HALVES>(a, st);
 }

@@ -8,8 +8,11 @@
 
 namespace reslim {
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_row;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_row;
+// 16 and 8 bytes from any address: one access of gfx950 whether or not it is a multiple of its size
+typedef __attribute__((ext_vector_type(4), aligned(1))) uint32_t u32x4_row;
+typedef __attribute__((ext_vector_type(2), aligned(1))) uint32_t u32x2_row;
+typedef uint32_t __attribute__((aligned(1))) u32_row;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_row;
 
 struct e4m3_t { uint8_t bits; };      // sign, 4 bits of exponent (bias 7), 3 of mantissa; largest 448, no infinities
 constexpr float kE4m3Max = 448.0f;
@@ -20,15 +23,15 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
 }
 
-// V consecutive elements; V > 1: the address is a multiple of V elements' bytes (at most 16)
+// V consecutive elements, from any element on
 template <class T, int V> struct Piece;
 template <int V> struct Piece<float, V> {
   static __device__ __forceinline__ void load(const float *p, float (&v)[V]) {
     if constexpr (V % 4 == 0) {
 #pragma unroll
       for (int i = 0; i < V; i += 4) {
-        const float4 f = *reinterpret_cast<const float4 *>(p + i);
-        v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+        const f32x4_row f = *reinterpret_cast<const f32x4_row *>(p + i);
+        v[i] = f[0]; v[i + 1] = f[1]; v[i + 2] = f[2]; v[i + 3] = f[3];
       }
     } else {
 #pragma unroll
@@ -38,7 +41,7 @@ template <int V> struct Piece<float, V> {
   static __device__ __forceinline__ void store(float *p, const float (&v)[V]) {
     if constexpr (V % 4 == 0) {
 #pragma unroll
-      for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4_row *>(p + i) = f32x4_row{v[i], v[i + 1], v[i + 2], v[i + 3]};
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i] = v[i];
@@ -56,7 +59,7 @@ template <int V> struct Piece<bf16_t, V> {
       const u32x2_row r = *reinterpret_cast<const u32x2_row *>(p);
       w[0] = r[0]; w[1] = r[1];
     } else if constexpr (V == 2) {
-      w[0] = *reinterpret_cast<const uint32_t *>(p);
+      w[0] = *reinterpret_cast<const u32_row *>(p);
     } else {
       w[0] = *p;
     }
@@ -69,7 +72,7 @@ template <int V> struct Piece<bf16_t, V> {
     } else if constexpr (V == 4) {
       *reinterpret_cast<u32x2_row *>(p) = u32x2_row{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     } else if constexpr (V == 2) {
-      *reinterpret_cast<uint32_t *>(p) = pack_bf16x2(v[0], v[1]);
+      *reinterpret_cast<u32_row *>(p) = pack_bf16x2(v[0], v[1]);
     } else {
       *p = f32_to_bf16(v[0]);
     }
@@ -80,7 +83,7 @@ template <int V> struct Piece<e4m3_t, V> {
     if constexpr (V == 8) {
       *reinterpret_cast<u32x2_row *>(p) = u32x2_row{pack_e4m3x4(v[0], v[1], v[2], v[3]), pack_e4m3x4(v[4], v[5], v[6], v[7])};
     } else if constexpr (V == 4) {
-      *reinterpret_cast<uint32_t *>(p) = pack_e4m3x4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<u32_row *>(p) = pack_e4m3x4(v[0], v[1], v[2], v[3]);
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i].bits = static_cast<uint8_t>(pack_e4m3x4(v[i], 0.f, 0.f, 0.f) & 0xff);
@@ -102,11 +105,18 @@ template <class T, int V> struct Held {
     } else if constexpr (kWords == 2) {
       const u32x2_row r = *reinterpret_cast<const u32x2_row *>(p);
       w[0] = r[0]; w[1] = r[1];
-    } else if constexpr (sizeof(T) == 4) {
-      w[0] = *reinterpret_cast<const uint32_t *>(p);
-    } else {
-      w[0] = *reinterpret_cast<const uint16_t *>(p);
     }
+    static_assert(kWords % 2 == 0, "whole pieces of 8 or 16 bytes");
+  }
+  __device__ __forceinline__ void load_some(const T *p, int n) {      // the first n
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) {
+        if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+        else w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << (i % 2 * 16);
+      }
   }
   __device__ __forceinline__ float operator[](int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
@@ -114,12 +124,24 @@ template <class T, int V> struct Held {
   }
 };
 
-// ... and as floats
-template <class T, int V> struct Loaded {
-  float v[V];
-  __device__ __forceinline__ void load(const T *p) { Piece<T, V>::load(p, v); }
-  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
-};
+// ... and the first n of V elements, zeros behind them
+template <class T, int V>
+__device__ __forceinline__ void load_some(const T *p, int n, float (&v)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float f[1] = {0.f};
+    if (i < n) Piece<T, 1>::load(p + i, f);
+    v[i] = f[0];
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ void store_some(T *p, int n, const float (&v)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float f[1] = {v[i]};
+    if (i < n) Piece<T, 1>::store(p + i, f);
+  }
+}
 
 // Sum (or maximum) over the NT threads that share a row, the same value in all of them.  box: NT / 64 floats of LDS that nothing
 // else uses until every thread is past the call after next (two boxes taken in turn).

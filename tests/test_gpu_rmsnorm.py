@@ -191,6 +191,25 @@ def test_rows_behind_two_to_the_31_elements():
         assert P.worst(dx[at], want, bound * 1.01 + P.half(H) * want.abs() + 1e-40) <= 1
 
 
+@pytest.mark.parametrize("stream,act", [(F, F), (F, H), (H, H)], ids=["f32", "f32_bf16", "bf16"])
+@pytest.mark.parametrize("D", [1, 3, 7, 61, 257, 1021, 2047, 4093, 8189, 9001, 16383])
+def test_a_row_that_ends_inside_a_piece_takes_nothing_from_the_next(D, stream, act):
+    rows = 2000 // (D // 1000 + 1)
+    x, delta, gamma = _inputs(rows, D, stream, act)
+    d_sum = torch.randn_like(x)
+    wild = torch.zeros(rows, 1, device="cuda")
+    wild[1::2], wild[3::4] = math.nan, math.inf
+    for yt in (act, Q):
+        clean, mixed = x.clone(), x + wild.to(stream)
+        for t in (clean, mixed):
+            t.y, t.scale = torch.empty(rows, D, dtype=yt, device="cuda"), torch.empty(rows, device="cuda") if yt == Q else None
+            B.reslim_rmsnorm_fwd(t, gamma, t.y, eps=EPS, delta=delta, sum_out=t, y_scale=t.scale)        # in place
+        for a, b in ((clean, mixed), (clean.y.view(torch.uint8), mixed.y.view(torch.uint8))) + (((clean.scale, mixed.scale),) if yt == Q else ()):
+            assert torch.equal(a[::2], b[::2])
+    clean, mixed = _backward(x, delta, gamma, d_sum, True), _backward(x + wild.to(stream), delta, gamma, d_sum + wild.to(stream), True)
+    assert torch.equal(clean[0][::2], mixed[0][::2]) and torch.equal(clean[1][::2], mixed[1][::2])
+
+
 def test_more_rows_than_a_launch_has_threads():
     n = 68_000_000                                   # a wave each: 4.35e9 threads
     x, y, scale = torch.ones(n, 64, dtype=H, device="cuda"), torch.zeros(n, 64, dtype=Q, device="cuda"), torch.zeros(n, device="cuda")
