@@ -1,10 +1,13 @@
 // The gated feed-forward layer's products on the fp32 path, for small problems and parity: any sizes, any operand order.
 //
 //   C[m, n] = sum_k A(m, k) B(n, k), fp32 matrix instructions (v_mfma_f32_32x32x2), tiles of 64 x 64 with a 32 x 32 block for each of
-// four waves, slabs of 32 k in two LDS buffers, the next slab's loads in flight in registers.  An operand whose k is contiguous is staged as
-// [row][k], one whose rows are as [k][row], both with 16-byte loads, so that one kernel serves the forward products, the gradients of their inputs (B
-// read across its rows) and of the weights (both read across).  Where there are few tiles, k is cut into slices that are added in
-// order.  A gated block is 16 gate and 16 up rows of the same features; lanes 16 apart exchange them.
+// four waves, slabs of 32 k in two LDS buffers, the slab after the next in flight in registers.  An operand whose k is contiguous is staged as
+// [row][k], one whose rows are as [k][row], so that one kernel serves the forward products, the gradients of their inputs (B
+// read across its rows) and of the weights (both read across, the bias gradient with them).  Where there are few tiles, k is cut into slices that
+// are added in order.  A gated block is 16 gate and 16 up rows of the same features; lanes 16 apart exchange them.
+//   The matrix instructions bound it: 16,384 x 2048 x 11,008 runs at 118 TFLOP/s, the library's 8192^3 at 153.  At 2048 x 512 x 1368 (one to four
+// work-groups a compute unit) the forward takes 102 us and the gradient 225: 48 us for the hidden layer's (60 TFLOP/s, its epilogue
+// moves 34 MB), 65 for the input's (88), 73 and 40 for the weights' (79, 72), 15 for the sums.
 #include <algorithm>
 #include <type_traits>
 
@@ -41,6 +44,7 @@ struct Slab {
   f32x4 v[2];
   const float *at[2];          // this thread's first values of slab 0: ALONG_K four k of two rows, else four rows at two k
   int64_t step;
+  int live;                    // k of the slab in v that exist, where not all do
   int k, last;                 // its first k in a slab; not ALONG_K: the last of its four rows that exists
   bool fours;                  // not ALONG_K: all or none of any thread's four rows exist
   template <class RowOf>
@@ -64,10 +68,11 @@ struct Slab {
   }
   __device__ __forceinline__ void load(int k0, int k_end) {
     const float *q[2];
+    live = k_end - k0;
+    if (live >= kBK) {                       // uniform
 #pragma unroll
-    for (int j = 0; j < 2; ++j) q[j] = ALONG_K ? at[j] + k0 : at[j] + k0 * step;
-    if (k0 + kBK <= k_end) {                 // uniform
-      if (ALONG_K || fours) {               // uniform
+      for (int j = 0; j < 2; ++j) q[j] = ALONG_K ? at[j] + k0 : at[j] + k0 * step;
+      if (ALONG_K || fours) {                // uniform
 #pragma unroll
         for (int j = 0; j < 2; ++j) v[j] = *reinterpret_cast<const f32x4_any *>(q[j]);
       } else {
@@ -76,15 +81,23 @@ struct Slab {
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[j][i] = q[j][min(i, last)];
       }
-    } else {
+    } else {                                 // k past the end: the last one, zero in LDS
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        q[j] = ALONG_K ? at[j] + k0 - k : at[j] + (k0 + min(0, live - 1 - k - 16 * j)) * step;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = q[j][ALONG_K ? min(k + i, live - 1) : min(i, last)];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float *lds) {
+    const int t = threadIdx.x;
+    if (live < kBK) {                        // uniform
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[j][i] = k0 + k + (ALONG_K ? i : 16 * j) < k_end ? q[j][ALONG_K ? i : min(i, last)] : 0.f;
+        for (int i = 0; i < 4; ++i) v[j][i] = k + (ALONG_K ? i : 16 * j) < live ? v[j][i] : 0.f;
     }
-  }
-  __device__ __forceinline__ void store(float *lds) const {
-    const int t = threadIdx.x;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       *reinterpret_cast<f32x4 *>(lds + (ALONG_K ? (t / 8 + 32 * j) * kPitchK + t % 8 * 4 : (t / 16 + 16 * j) * kPitchRow + t % 16 * 4)) = v[j];
@@ -273,10 +286,11 @@ __global__ __launch_bounds__(256) void gated_f32_sum_kernel(const float *__restr
   }
 }
 
-// Slices of k: as many as fill the four work-groups that a compute unit holds, of at least eight slabs each.
+// Slices of k: as many as fill the four work-groups that a compute unit holds, of at least three slabs each: a slab takes an empty chip about
+// 1 us, the launch that adds the slices 2 to 5 (gradient of 673 x 83 x 363 46 us; with eight slabs 68, with two 45, but 69 for 65 at 3700 x 100 x 300).
 int f32_slices(int M, int N, int K) {
   const int64_t tiles = (static_cast<int64_t>(M) + kTile - 1) / kTile * ((static_cast<int64_t>(N) + kTile - 1) / kTile);
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, K / (8 * kBK))));
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, K / (3 * kBK))));
 }
 size_t slice_bytes(int M, int N, int K, int more) {      // more: floats of a slice beside the product
   const int s = f32_slices(M, N, K);
