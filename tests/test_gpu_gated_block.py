@@ -16,6 +16,15 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-6
 
 
+@pytest.fixture(autouse=True)
+def _float32():
+    """Other modules make float64 torch's default for the whole session."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 def _reference(stream, delta, p, pos, freq, tiles, heads, gate, d_out):
     """Block in float64 on the leaves p; returns (stream out, last delta, gradients of everything)."""
     leaves = {n: t.double().detach().requires_grad_() for n, t in p.items()}

@@ -12,6 +12,15 @@ pytestmark = pytest.mark.gpu
 F, H, Q = torch.float32, torch.bfloat16, torch.float8_e4m3fn
 
 
+@pytest.fixture(autouse=True)
+def _float32():
+    """Other modules make float64 torch's default for the whole session."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 def _gen(*seed):
     return torch.Generator(device="cuda").manual_seed(sum(s * 1000003 ** i for i, s in enumerate(seed)) % (1 << 40))
 

@@ -14,6 +14,15 @@ EPS = 1e-6
 WIDTHS = [1, 3, 4, 8, 60, 64, 65, 100, 256, 257, 260, 512, 895, 1000, 1024, 1025, 1032, 2048, 2056, 4096, 4097, 4104, 8192, 8200, 16383, 16384]
 
 
+@pytest.fixture(autouse=True)
+def _float32():
+    """Other modules make float64 torch's default for the whole session."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 def _off(t, n):
     """The same values `n` elements into an allocation."""
     return torch.empty(t.numel() + n, dtype=t.dtype, device="cuda")[n:].view(t.shape).copy_(t)

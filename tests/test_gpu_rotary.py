@@ -12,6 +12,15 @@ pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
 
 
+@pytest.fixture(autouse=True)
+def _float32():
+    """Other modules make float64 torch's default for the whole session."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 def _table(rot, axes, **kw):
     f, amp = B.reslim_rotary_frequencies(rot, axes, **kw)
     return torch.from_numpy(f).cuda(), amp
