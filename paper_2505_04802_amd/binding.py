@@ -719,25 +719,32 @@ def reslim_rotary_frequencies(rot: int, axes: int = 1, base: float = 10000.0, sc
     return freq, float(amplitude.value)
 
 
+def _heads_of(name: str, t, heads: int, dev):
+    """(tokens, elements from token to token, features of a head) of [tokens, heads or more, features] with contiguous heads."""
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] < heads or (shape[0] > 0 and (strides[2] != 1 or strides[1] != shape[2])):
+        raise ValueError(f"{name} must be [tokens, at least {heads} heads, dh] with contiguous heads: got {tuple(shape)}, strides {strides}")
+    # the stride of a dimension of one token says nothing
+    return shape[0], strides[0] if shape[0] > 1 else shape[1] * shape[2], shape[2]
+
+
 def _rotary(call, x, out, positions, freq, heads, layout, amplitude, stream):
     import torch
     if layout not in ROTARY_LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(ROTARY_LAYOUTS)}")
     dev, st = _current()
-    for name, t in (("x", x), ("out", out)):
-        if t.get_device() != dev:
-            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
-        if t.dim() != 3 or t.shape[1] < heads or (t.shape[0] > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):
-            raise ValueError(f"{name} must be [tokens, at least {heads} heads, dh] with contiguous heads: got {tuple(t.shape)}, strides {tuple(t.stride())}")
-    tokens, _, dh = x.shape
-    if out.dtype is not x.dtype or out.shape[0] != tokens or out.shape[2] != dh:
-        raise ValueError(f"out must match x in type, tokens and head size: {out.dtype} {tuple(out.shape)} for {x.dtype} {tuple(x.shape)}")
-    axes, period = _rows_of("positions", positions, dev)
+    tokens, xs, dh = _heads_of("x", x, heads, dev)
+    out_s = xs
+    if out is not x:
+        n, out_s, d = _heads_of("out", out, heads, dev)
+        if out.dtype is not x.dtype or n != tokens or d != dh:
+            raise ValueError(f"out must match x in type, tokens and head size: {out.dtype} {tuple(out.shape)} for {x.dtype} {tuple(x.shape)}")
+    axes, period = shape = _rows_of("positions", positions, dev)
     pairs = freq.numel()
-    # the stride of a dimension of one token says nothing
-    xs, os = (t.stride(0) if tokens > 1 else t.shape[1] * dh for t in (x, out))
-    _check(call(x.data_ptr(), out.data_ptr(), _fits("positions", positions, (axes, period), torch.int32, dev), _fits("freq", freq, (pairs,), torch.float64, dev),
-                tokens, xs, os, period, heads, dh, 2 * pairs, axes, ROTARY_LAYOUTS[layout], amplitude, _code(x.dtype), st if stream is None else stream.cuda_stream))
+    _check(call(x.data_ptr(), out.data_ptr(), _fits("positions", positions, shape, torch.int32, dev), _fits("freq", freq, (pairs,), torch.float64, dev),
+                tokens, xs, out_s, period, heads, dh, 2 * pairs, axes, ROTARY_LAYOUTS[layout], amplitude, _code(x.dtype), st if stream is None else stream.cuda_stream))
 
 
 def reslim_rotary_fwd(x, out, positions, freq, *, heads: int, layout: str = "half", amplitude: float = 1.0, stream=None) -> None:
