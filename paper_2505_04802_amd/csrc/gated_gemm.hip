@@ -545,7 +545,14 @@ GatedChoice gated_choose_dgate(int M, int D, int R, double other) { return gated
 hipError_t launch_gated_out(const GatedChoice &how, const void *a, const void *w, bool across, const float *bias, const float *zeros, void *out, int M, int N, int K, float *part,
                             hipStream_t st) {
   if (M <= 0 || N <= 0 || K <= 0 || K % 64 || N % 64 || (across && how.kernel != kGatedRing)) return hipErrorInvalidValue;
-  if (how.slices == 1 && how.kernel != kGatedRing) return launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, a, w, bias ? bias : zeros, out, N, nullptr, 0, M, N, K, st);
+  if (how.slices == 1 && how.kernel != kGatedRing) {
+    const int whole = how.kernel == kGemm256x256 ? gated_whole_rounds(M, N, K / 64, kEpiAct, g_num_cus) : M;
+    const hipError_t e = launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, a, w, bias ? bias : zeros, out, N, nullptr, 0, whole, N, K, st);
+    if (e != hipSuccess || whole == M) return e;
+    const int64_t at = whole;
+    return launch_gated_out(gated_choose(M - whole, N, N, K / 64, kEpiAct, g_num_cus, false, false, 0.0), static_cast<const bf16_t *>(a) + at * K, w, false, bias, zeros,
+                            static_cast<bf16_t *>(out) + at * N, M - whole, N, K, nullptr, st);
+  }
   GemmArgs g = {};
   g.A = a; g.W = w; g.bias = bias; g.out = out; g.ldo = N; g.tab_rows = 1; g.M = M; g.N = N; g.K = K;
   if (how.slices == 1) return across ? launch_ring<EPI_BIAS_ACT, true>(g, st) : launch_ring<EPI_BIAS_ACT>(g, st);

@@ -46,4 +46,16 @@ inline GatedChoice gated_choose(int M, int N, int cols, int slabs, GemmEpi epi, 
   return best;
 }
 
+// Rows of a product on 256 x 256 tiles that fill whole rounds of them, where the rows of the last, part-filled round are faster in a launch of
+// their own (any kernel, no slices) by 5 % of the whole; else all rows.  Every kernel sums k in the same order, so the result does not depend on it.
+// Layers in one launch and in two: 17,000 x 2048 x 8192 1373 and 1276 us, 9000 x 4096 x 2752 534 and 522, 40,352 x 1024 x 2752 588 and 576, its
+// gradient 1416 and 1391; where 3 % are promised (80,704 x 1536 x 2752) two lose up to 1 %.
+inline int gated_whole_rounds(int M, int N, int slabs, GemmEpi epi, int cus) {
+  const int64_t across = (N + 255) / 256, rounds = (M + int64_t{255}) / 256 * across / cus, rows = rounds * cus / across * 256;
+  if (rounds < 1 || rows >= M) return M;
+  const int whole = static_cast<int>(rows);
+  const double all = gemm_times(M, N, slabs * 64, epi, cus).pp2, part = gemm_times(whole, N, slabs * 64, epi, cus).pp2;
+  return part + gated_choose(M - whole, N, N, slabs, epi, cus, false, false, 0.0).us + 2.0 < 0.95 * all ? whole : M;
+}
+
 }  // namespace reslim

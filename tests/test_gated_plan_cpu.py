@@ -22,6 +22,7 @@ extern "C" int choose(int M, int N, int cols, int slabs, int epi, int sliceable,
   *slices = c.slices;
   return c.us > 0 ? c.kernel : -1;
 }
+extern "C" int whole(int M, int N, int slabs) { return gated_whole_rounds(M, N, slabs, kEpiAct, 256); }
 """
 RING, SMALL, WIDE, TALL = 1, 2, 3, 4      # 64 x 64; one 128 x 128 tile a work-group; persistent 256 x 256; 128 x 256
 ACT, GELU, TWO, F32, STREAM = range(5)
@@ -40,6 +41,7 @@ def choose(tmp_path_factory):
         s = ctypes.c_int(0)
         return lib.choose(M, N, cols, slabs, epi, sliceable, e4m3, other, ctypes.byref(s)), s.value
 
+    ask.whole = lib.whole
     return ask
 
 
@@ -110,3 +112,23 @@ def test_nothing_touches_a_read_in_flight():
         if "gemm_ring_kernel" in name:
             assert any("vmcnt(8)" in l for l in lines), name
     assert kernels == 4          # dx whole and in slices, and the gate gradient with either activation
+
+
+def test_rows_of_whole_rounds(choose):
+    """The split is at a whole number of 256 x 256 tiles' rounds, and is made where it was measured to pay."""
+    r = random.Random(2)
+    split = 0
+    for _ in range(4000):
+        M, N, slabs = int(2 ** r.uniform(8, 18)), 64 * int(2 ** r.uniform(0, 8)), int(2 ** r.uniform(0, 8))
+        rows = choose.whole(M, N, slabs)
+        assert 0 < rows <= M
+        if rows < M:
+            split += 1
+            assert rows % 256 == 0 and rows // 256 * -(-N // 256) <= -(-M // 256) * -(-N // 256) // 256 * 256
+    assert split > 20
+    for rows, K, kernel in ((16500, 1024, RING), (18000, 1024, SMALL), (16500, 2048, RING), (18000, 2048, SMALL), (20000, 2048, TALL)):      # the GPU test's
+        assert choose.whole(rows, 2048, K // 64) == 16384 and choose(rows - 16384, 2048, 2048, K // 64, ACT)[0] == kernel
+    # products of the layer's output map, microseconds of the layer in one launch and in two: 40,352 x 1024 x 2752 588 and 576, 17,000 x 2048 x 8192 1373 and
+    # 1276, 20,000 x 2048 x 5504 1053 and 1034; the last two: within the noise
+    for (M, N, K), pays in {(40352, 1024, 2752): True, (17000, 2048, 8192): True, (20000, 2048, 5504): True, (80704, 1024, 2752): False, (80704, 1536, 2752): False}.items():
+        assert (choose.whole(M, N, K // 64) < M) == pays, (M, N, K)

@@ -174,6 +174,25 @@ def test_many_rows_go_through_the_persistent_kernels():
     _near(_forward(x8, w8, H, "gelu", xs), want["y"], want["y_bound"], H, "y of e4m3")
 
 
+@pytest.mark.parametrize("rows", [16500, 18000, 20000])
+def test_rows_past_the_whole_rounds_of_tiles(rows):
+    """The output map's product and the input gradient's are cut behind row 16,384, for either of the three kernels that the rest may get."""
+    D, R = 2048, 1024
+    x, _, w = _case(rows, D, R, H, True)
+    gu, h, y = _train(x, w, "silu")
+    dy = torch.randn(rows, D, generator=_gen(rows), device="cuda").to(H)
+    got = _backward(x, gu, h, dy, w, "silu", H)
+    at = torch.cat([torch.arange(0, 40), torch.arange(16384 - 40, 16384 + 100), torch.arange(rows - 40, rows)]).cuda()
+    want = P.gated_mlp(x[at], w, "silu", H)
+    _near(y[at], want["y"], want["y_bound"], H, "y")
+    want = P.gated_mlp_bwd(x[at], gu[at], h[at], dy[at], w, "silu", H, H)
+    assert P.worst(got["dx"][at], want["dx"], want["dx_bound"] * 1.01 + 1e-30) <= 1
+    cut = 16384 + 64
+    for rest in (slice(0, cut), slice(cut - 300, rows)):      # whole and part again, in calls that are cut elsewhere: the same bits
+        a, b = _train(x[rest].contiguous(), w, "silu"), (gu[rest], h[rest])
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("x_type,rows", [(H, 3), (H, 70), (H, 700), (F, 70), (Q, 3), (Q, 70)])
 def test_a_row_does_not_touch_others_and_nothing_behind_the_last_is_written(x_type, rows):
     act = F if x_type == F else H
