@@ -191,6 +191,8 @@ hipError_t launch_gemm(int dtype, Epilogue epi, const void *A, const void *W, co
                        void *out, int ldo, const float *tab, int tab_rows, int M, int N, int K,
                        hipStream_t st, float qscale = 1.0f, int qcols = 0, const void *aux = nullptr, void *out2 = nullptr,
                        const ResRowMap *res_map = nullptr);
+// out [M, N] bf16 = A W^T + bias on the kernel that the caller has chosen (a GemmKernel; the debugging hook overrules it)
+hipError_t launch_gemm_act(int kernel, const void *A, const void *W, const float *bias, void *out, int M, int N, int K, hipStream_t st);
 // aux: EPI_BIAS_RES_F32: float skip input, [M, ldo] or the rows res_map names.  out2: EPI_BIAS_ACT_GELU2: act [M, ldo].
 // out = LayerNorm(x) W^T (+ epilogue) in one launch, fp32 path: rows of up to 256 features while the outputs are few; `rows`: which rows of x
 bool gemm_takes_layernorm(int dtype, const void *A, const void *W, const float *ln_g, const float *ln_b, int M, int N, int K);

@@ -547,7 +547,7 @@ hipError_t launch_gated_out(const GatedChoice &how, const void *a, const void *w
   if (M <= 0 || N <= 0 || K <= 0 || K % 64 || N % 64 || (across && how.kernel != kGatedRing)) return hipErrorInvalidValue;
   if (how.slices == 1 && how.kernel != kGatedRing) {
     const int whole = how.kernel == kGemm256x256 ? gated_whole_rounds(M, N, K / 64, kEpiAct, g_num_cus) : M;
-    const hipError_t e = launch_gemm(RESLIM_BF16, EPI_BIAS_ACT, a, w, bias ? bias : zeros, out, N, nullptr, 0, whole, N, K, st);
+    const hipError_t e = launch_gemm_act(how.kernel, a, w, bias ? bias : zeros, out, whole, N, K, st);
     if (e != hipSuccess || whole == M) return e;
     const int64_t at = whole;
     return launch_gated_out(gated_choose(M - whole, N, N, K / 64, kEpiAct, g_num_cus, false, false, 0.0), static_cast<const bf16_t *>(a) + at * K, w, false, bias, zeros,

@@ -18,9 +18,13 @@ constexpr double kMostTiles = 1 << 23;      // work-groups of 256 threads that o
 // a work-group 0.26 us, its latency over the three in flight, while two lie on a compute unit, and a compute unit 0.27, what it draws
 // from L2 for one.  Slices of k make more work-groups of shorter sums, at the price of a second launch and of partial sums that are read
 // again.  gemm_times is fitted to products whose weights lie in a cache; a model's come from memory, and where every work-group has one tile a slab
-// then takes a persistent kernel 0.8 us (128 x 256) and 1.35 (256 x 256): 64 x 4096 x 10,944 140 us instead of 79.  N: rows of W that are read
-// (both matrices of a gated product); cols: columns of the result; slabs: K in slabs of 128 bytes a row; other: what the kernels
-// beside the ring cost on top (copies of weights that it does without).
+// then takes a persistent kernel 0.8 us (128 x 256) and 1.35 (256 x 256): 64 x 4096 x 10,944 140 us instead of 79.
+//   Whole products of the output map and of dx that neither the ring nor slices win are hundreds of tiles reading the same rows of W, and there 0.8 and 1.35 us
+// overrate memory: of 95 with cold weights the kernel that they would choose is 0.6 % slower than the best of the three, 1448 x 2112 x 4864 120 us instead of
+// 115, the choice by gemm_times itself 0.4 %.  So that is what these get; where it sees no difference (0.2 %) between kernels with a tile or less for a
+// compute unit, as at 1616 x 2048 x 2048 (62.6 and 62.4 us), 128 x 128, which leaves the launches around it their clock.
+//   N: rows of W that are read (both matrices of a gated product); cols: columns of the result; slabs: K in slabs of 128 bytes a row; other: what the
+// kernels beside the ring cost on top (copies of weights that it does without).
 inline GatedChoice gated_choose(int M, int N, int cols, int slabs, GemmEpi epi, int cus, bool sliceable, bool e4m3, double other) {
   constexpr double ring_epi[] = {0.8, 1.0, 1.5, 1.0, 2.0};
   const GemmTimes g = gemm_times(M, N, slabs * 64, epi, cus);
@@ -42,6 +46,10 @@ inline GatedChoice gated_choose(int M, int N, int cols, int slabs, GemmEpi epi, 
       const double ws = mid * n / cus, fs = std::min(1.0, std::max(0.0, (0.62 * std::ceil(ws) + 0.38 * ws - 1.0) / 2.0));
       offer(kGemm128, n, per * (0.73 + 1.07 * fs) + 5.99 * (0.12 + 0.88 * fs) + add + other);
     }
+  }
+  if (!e4m3 && epi == kEpiAct && best.kernel != kGatedRing && best.slices == 1) {
+    const double persistent = std::min(g.pp1, g.pp2), tie = count(128, 256) <= cus ? 0.998 : 1.0;
+    best.kernel = mid <= kMostTiles && tie * g.small <= persistent ? kGemm128 : g.pp1 < g.pp2 ? kGemm128x256 : kGemm256x256;
   }
   return best;
 }

@@ -374,13 +374,15 @@ static constexpr GemmEpi epi_cost() {
 }
 
 template <int EPI>
-static hipError_t launch_bf16(GemmArgs g, hipStream_t st) {
-  switch (g_gemm_tile_override >= 0 ? g_gemm_tile_override : gemm_choose(g.M, g.N, g.K, epi_cost<EPI>(), g_num_cus)) {
+static hipError_t launch_bf16(GemmArgs g, int kernel, hipStream_t st) {
+  switch (g_gemm_tile_override >= 0 ? g_gemm_tile_override : kernel) {
     case kGemm256x256: return launch_bf16_pp<2, EPI>(g, st);
     case kGemm128x256: return launch_bf16_pp<1, EPI>(g, st);
     default: return launch_bf16_tc<TileSmall, EPI>(g, st);
   }
 }
+template <int EPI>
+static hipError_t launch_bf16(const GemmArgs &g, hipStream_t st) { return launch_bf16<EPI>(g, gemm_choose(g.M, g.N, g.K, epi_cost<EPI>(), g_num_cus), st); }
 
 static bool f32_split(int M, int N) {      // four waves to a 32 x 32 tile
   return static_cast<int64_t>((M + 31) / 32) * ((N + 31) / 32) < 8LL * g_num_cus;
@@ -445,6 +447,14 @@ hipError_t gemm_init() {
   if ((e = init_epi<EPI_BIAS_ACT_GELU2>()) != hipSuccess) return e;
   if ((e = init_epi<EPI_BIAS_RES_F32>()) != hipSuccess) return e;
   return init_epi<EPI_BIAS_F32>();
+}
+
+hipError_t launch_gemm_act(int kernel, const void *A, const void *W, const float *bias, void *out, int M, int N, int K, hipStream_t st) {
+  if (M <= 0 || N <= 0 || K <= 0 || K % 64 != 0 || N % 8 != 0) return hipErrorInvalidValue;
+  GemmArgs g = {};
+  g.A = A; g.W = W; g.bias = bias; g.out = out; g.ldo = N; g.tab_rows = 1; g.M = M; g.N = N; g.K = K;
+  g.col_fast = g_col_fast; g.qscale = 1.0f; g.res_out = 1;
+  return launch_bf16<EPI_BIAS_ACT>(g, kernel, st);
 }
 
 hipError_t launch_gemm(int dtype, Epilogue epi, const void *A, const void *W, const float *bias,

@@ -1,0 +1,89 @@
+"""What the gated feed-forward layer launches (a stand-in for the HIP runtime notes it; nothing runs) against what csrc/gated_plan.h plans."""
+import ctypes
+import os
+import random
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from launch_record import ask
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_04802_amd", "csrc")
+PLAN = r"""
+#include "gated_plan.h"
+using namespace reslim;
+extern "C" int choose(int M, int N, int slabs, int sliceable, double other, int *slices) {
+  const GatedChoice c = gated_choose(M, N, N, slabs, kEpiAct, 256, sliceable, false, other);
+  *slices = c.slices;
+  return c.kernel;
+}
+extern "C" int whole(int M, int N, int slabs) { return gated_whole_rounds(M, N, slabs, kEpiAct, 256); }
+"""
+RING, SMALL, WIDE, TALL = 1, 2, 3, 4
+BF16 = 1
+CALLS = """
+for M, D, R in sizes:
+    rc = [lib.reslim_gated_mlp_fwd(p, None, gated_weights(), 0, M, D, R, 1, p, p, 1 << 40, None)]
+    fwd = launches()
+    rc.append(lib.reslim_gated_mlp_bwd(p, p, p, p, gated_weights(), 0, M, D, R, 1, 1, p, GRADS, p, 1 << 40, None))
+    out.append((rc, fwd, launches()))
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cc = shutil.which("g++") or pytest.skip("no g++")
+    d = tmp_path_factory.mktemp("plan")
+    (d / "ask.cpp").write_text(PLAN)
+    subprocess.run([cc, "-O2", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(d / "ask.cpp"), "-o", str(d / "ask.so")], check=True)
+    lib = ctypes.CDLL(str(d / "ask.so"))
+    lib.choose.argtypes = [ctypes.c_int] * 4 + [ctypes.c_double, ctypes.POINTER(ctypes.c_int)]
+
+    def planned(M, N, K, other):
+        """[(kernel, slices, rows)] of one product."""
+        s = ctypes.c_int(0)
+        kernel = lib.choose(M, N, K // 64, 1, other, ctypes.byref(s))
+        rows = lib.whole(M, N, K // 64) if kernel == WIDE else M
+        if rows == M:
+            return [(kernel, s.value, M)]
+        return [(WIDE, 1, rows), (lib.choose(M - rows, N, K // 64, 0, 0.0, ctypes.byref(s)), 1, M - rows)]
+
+    return planned
+
+
+def _products(launched):
+    """[(kernel, slices)] of the products with plain or sliced results among the launches: epilogues 0 and 96."""
+    found = []
+    for name, grid in launched:
+        m = re.match(r"void (gemm_ring_kernel|gemm_bf16_pp_kernel|gemm_bf16_kernel)<(.*?)>", name)
+        if not m:
+            continue
+        args = [int(a) if a.strip().isdigit() else a.strip() for a in m[2].split(",")]
+        epi = args[0] if m[1] == "gemm_ring_kernel" else args[-1]
+        if epi in (0, 96):
+            found.append((RING if m[1] == "gemm_ring_kernel" else SMALL if m[1] == "gemm_bf16_kernel" else {2: WIDE, 1: TALL}[args[0]], grid[1]))
+    return found
+
+
+def _sizes():
+    r, sizes = random.Random(3), [(16500, 2048, 1024), (18000, 2048, 1024), (20000, 2048, 1024), (2323, 1344, 3840), (1448, 2112, 4864), (1431, 2368, 1728), (40352, 1024, 2752)]
+    while len(sizes) < 1500:
+        M, D, R = int(2 ** r.uniform(0, 16.5)), 64 * int(2 ** r.uniform(0, 6)), 64 * int(2 ** r.uniform(0, 7.5))
+        if M * D * R < 2e12:
+            sizes.append((M, D, R))
+    return sizes
+
+
+def test_the_planned_kernels_are_launched(plan, tmp_path_factory):
+    sizes, kinds = _sizes(), {"out": set(), "dx": set()}
+    for (M, D, R), (rc, fwd, bwd) in zip(sizes, ask(tmp_path_factory, CALLS, sizes=sizes)):
+        assert rc == [0, 0]
+        copy = 4e-6 / 4.5 * D * R
+        for what, launched, want in (("out", fwd, plan(M, D, R, 0.0)), ("dx", bwd, plan(M, D, 2 * R, 2.0 + 2 * copy))):
+            assert _products(launched) == [(k, s) for k, s, _ in want], (what, M, D, R, want)
+            kinds[what].add((want[0][0], want[0][1] > 1, len(want), want[-1][0]))
+    for what, met in kinds.items():      # whole products of every kernel, slices, and rows of a last round
+        assert {(RING, True, 1, RING), (SMALL, True, 1, SMALL), (SMALL, False, 1, SMALL), (WIDE, False, 1, WIDE), (TALL, False, 1, TALL)} <= met, (what, met)
+        assert any(n == 2 for _, _, n, _ in met), (what, met)
