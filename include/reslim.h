@@ -646,7 +646,9 @@ int reslim_rotary_frequencies(int32_t rot, int32_t axes, double base, int32_t sc
  *   w_out act [D, R];  b_in float [2R], b_out float [D], either may be NULL
  * Types: x_dtype F32 (act float), BF16 (act bfloat16) or E4M3 (act bfloat16; forward only): x rows with x_scale float [rows] as
  * reslim_rmsnorm_fwd writes them.  rows <= 2,000,000,000, D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
- * sizes, rows <= 4,000,000 and at most 2^23 tiles of 64 rows by 32 of R, or 64 of D.  BF16 and E4M3 buffers start on 16 bytes. */
+ * sizes, rows <= 4,000,000 and at most 2^23 tiles of 64 rows by 32 of R, or 64 of D.  BF16 and E4M3 buffers start on 16 bytes.
+ * With act bfloat16 GELU is good to 1.5e-5 of its value, below -5 to 1.6e-3, and 0 below -14.  act(+inf) = inf; act(-inf) and act' at either infinity are
+ * NaN, as the formulas g / (1 + e^-g) and g Phi(g) and their derivatives give in fp32. */
 enum { RESLIM_GATE_SILU = 0, RESLIM_GATE_GELU = 1 };
 typedef struct {
   const void *w_in;

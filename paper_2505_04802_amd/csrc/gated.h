@@ -2,56 +2,12 @@
 // gated.hip holds the entry points, gated_gemm.hip the bf16 and e4m3 products, gated_f32.hip the fp32 path.
 #pragma once
 
+#include "gate_act.h"
 #include "gated_plan.h"
 #include "gelu.h"
 #include "rows_common.h"
 
 namespace reslim {
-
-// act(v) and its derivative to about 2e-6 of the larger of the two, for results that are rounded to bf16; NaN stays NaN.
-// SiLU: v p, p = 1 / (1 + e^-v); slope p + v p (1 - p).  GELU: v Phi(v), slope Phi(v) + v phi(v), Phi(-|v|) = 2^P(|v|) as in gelu.h.
-template <bool GELU>
-__device__ __forceinline__ float gate_act(float v) {
-  if constexpr (GELU) return gelu_erf_fast(v) + (v != v ? v : 0.f);      // that function's bounds drop a NaN
-  else return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
-}
-template <bool GELU>
-__device__ __forceinline__ void gate_act_slope(float v, float &a, float &slope) {
-  if constexpr (GELU) {
-    const float u = __builtin_amdgcn_fmed3f(fabsf(v), 0.0f, 5.0f);
-    float p = fmaf(2.975744064e-05f, u, -7.135751075e-04f);
-    p = fmaf(p, u, 7.775241509e-03f);
-    p = fmaf(p, u, -5.269032717e-02f);
-    p = fmaf(p, u, -4.595123231e-01f);
-    p = fmaf(p, u, -1.150926590e+00f);
-    p = fmaf(p, u, -1.000011683e+00f);
-    const float tail = __builtin_amdgcn_exp2f(p);
-    a = fmaf(-u, tail, v < 0.f ? 0.f : v);
-    slope = fmaf(v * 0.3989422804014327f, __builtin_amdgcn_exp2f(v * v * -0.72134752044448170f), v < 0.f ? tail : 1.0f - tail);
-  } else {
-    const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
-    a = v * p;
-    slope = fmaf(a, 1.0f - p, p);
-  }
-}
-// The same with the library's functions, for fp32 results.
-template <bool GELU>
-__device__ __forceinline__ void gate_act_slope_f32(float v, float &a, float &slope) {
-  if constexpr (GELU) {
-    const float p = 0.5f * (1.0f + erff(v * 0.70710678118654752f));
-    a = v * p;
-    slope = fmaf(v * 0.3989422804014327f, expf(-0.5f * v * v), p);
-  } else {
-    const float p = 1.0f / (1.0f + expf(-v));
-    a = v * p;
-    slope = fmaf(a, 1.0f - p, p);
-  }
-}
-template <bool GELU>
-__device__ __forceinline__ float gate_act_f32(float v) {
-  if constexpr (GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-  else return v / (1.0f + expf(-v));
-}
 
 struct GatedIn {                       // x W_in^T and what follows up to the hidden layer
   const void *x, *w_in;                // [M, D], [2R, D]: bf16 or e4m3
