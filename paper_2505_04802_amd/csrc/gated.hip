@@ -52,11 +52,20 @@ __global__ __launch_bounds__(256) void gated_zero_kernel(ZeroArgs a) {
 static size_t gated_hidden_bytes(int M, int R, int x_dtype) { return align256(static_cast<size_t>(M) * R * (x_dtype == RESLIM_F32 ? 4 : 2)); }
 // partial sums of a product's slices: out [M, N] over K
 static size_t gated_part_bytes(int slices, int M, int N) { return slices > 1 ? align256(static_cast<size_t>(slices) * M * N * sizeof(float)) : 0; }
-static size_t gated_out_bytes(int M, int D, int R, int x_dtype) {
-  if (M < 1) return 0;
-  return x_dtype == RESLIM_F32 ? gated_f32_product_bytes(M, D, R) : gated_part_bytes(gated_choose_out(M, D, R, 0.0).slices, M, D);
+// How the output map is computed, and the forward's workspace: partial sums, behind them the hidden layer.  Both go by the device's compute units: one
+// plan for the size that is checked and the launches, made after gated_ready.
+struct GatedFwdPlan {
+  GatedChoice out;
+  size_t hidden_at, total;
+};
+static GatedFwdPlan gated_fwd_plan(int M, int D, int R, int x_dtype) {
+  GatedFwdPlan p = {};
+  if (M < 1) return p;
+  if (x_dtype != RESLIM_F32) p.out = gated_choose_out(M, D, R, 0.0);
+  p.hidden_at = x_dtype == RESLIM_F32 ? gated_f32_product_bytes(M, D, R) : gated_part_bytes(p.out.slices, M, D);
+  p.total = p.hidden_at + gated_hidden_bytes(M, R, x_dtype);
+  return p;
 }
-static size_t gated_fwd_bytes(int M, int D, int R, int x_dtype) { return gated_out_bytes(M, D, R, x_dtype) + gated_hidden_bytes(M, R, x_dtype); }
 
 // How the two input gradients of the bf16 path are computed.  The 64 x 64 tiles read the weights as they lie; for the other kernels they are copied
 // transposed first, read and written once at about 4.5 TB/s, after the launch.
@@ -66,6 +75,7 @@ static GatedBwdPlan gated_bwd_plan(int M, int D, int R) {
   return {gated_choose_dgate(M, D, R, 2.0 + copy), gated_choose_out(M, D, 2 * R, 2.0 + 2 * copy)};
 }
 struct GatedBwdWs {
+  GatedBwdPlan plan;           // bf16
   void *d_gu;                  // act [M, 2R]
   void *wt_in, *wt_out;        // bf16 [D, 2R], [R, D], or null
   void *part;                  // partial sums of dx
@@ -86,10 +96,10 @@ static GatedBwdWs plan_gated_bwd(int M, int D, int R, int dtype, void *base) {
   if (M < 1) return w;
   w.d_gu = take(m * 2 * r * es);
   if (dtype == RESLIM_BF16) {
-    const GatedBwdPlan plan = gated_bwd_plan(M, D, R);
-    w.part = take(gated_part_bytes(plan.dx.slices, M, D));
-    if (plan.dx.kernel != kGatedRing) w.wt_in = take(2 * r * d * 2);
-    if (plan.dgate.kernel != kGatedRing) w.wt_out = take(r * d * 2);
+    w.plan = gated_bwd_plan(M, D, R);
+    w.part = take(gated_part_bytes(w.plan.dx.slices, M, D));
+    if (w.plan.dx.kernel != kGatedRing) w.wt_in = take(2 * r * d * 2);
+    if (w.plan.dgate.kernel != kGatedRing) w.wt_out = take(r * d * 2);
     w.sink_in = take(2 * r * sizeof(float));
     w.sink_out = take(d * sizeof(float));
     WgradOp op[2];
@@ -137,12 +147,12 @@ static int gated_room(const char *fn, const void *ws, size_t ws_bytes, size_t ne
   return refuse(RESLIM_EWORKSPACE, fn, "workspace null, not 256-byte aligned or smaller than the workspace query says");
 }
 
-static hipError_t gated_forward(const GatedIn &in, const reslim_gated_mlp_weights *w, int x_dtype, bool gelu, void *y, void *part, const float *zeros, hipStream_t st) {
+static hipError_t gated_forward(const GatedFwdPlan &plan, const GatedIn &in, const reslim_gated_mlp_weights *w, int x_dtype, bool gelu, void *y, void *part, const float *zeros, hipStream_t st) {
   const bool f32 = x_dtype == RESLIM_F32;
   const hipError_t e = f32 ? launch_gated_f32_in(in, gelu, st) : launch_gated_in(in, gelu, st);
   if (e != hipSuccess) return e;
   if (f32) return launch_gated_f32_out(static_cast<const float *>(in.h), static_cast<const float *>(w->w_out), w->b_out, static_cast<float *>(y), in.M, in.D, in.R, static_cast<float *>(part), st);
-  return launch_gated_out(gated_choose_out(in.M, in.D, in.R, 0.0), in.h, w->w_out, false, w->b_out, zeros, y, in.M, in.D, in.R, static_cast<float *>(part), st);
+  return launch_gated_out(plan.out, in.h, w->w_out, false, w->b_out, zeros, y, in.M, in.D, in.R, static_cast<float *>(part), st);
 }
 
 }  // namespace reslim
@@ -156,7 +166,7 @@ extern "C" int reslim_gated_mlp_workspace_bytes(int32_t rows, int32_t D, int32_t
   if (rc != RESLIM_OK) return rc;
   const float *zeros = nullptr;
   if (x_dtype != RESLIM_F32) (void)gated_ready(&zeros);      // the slices go by the device's compute units
-  *out = gated_fwd_bytes(rows, D, R, x_dtype);
+  *out = gated_fwd_plan(rows, D, R, x_dtype).total;
   return RESLIM_OK;
 }
 
@@ -167,13 +177,14 @@ extern "C" int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const r
   if (rc != RESLIM_OK) return rc;
   if (rows > 0 && (x_dtype == RESLIM_E4M3) != (x_scale != nullptr)) return refuse(RESLIM_EINVAL, fn, "x_scale goes with RESLIM_E4M3, and only with it");
   if (!aligned(x_scale, 4)) return refuse(RESLIM_EINVAL, fn, "a buffer is not aligned to its elements");
-  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, D, R, x_dtype))) != RESLIM_OK) return rc;
   if (rows == 0) return RESLIM_OK;
   const float *zeros = nullptr;
   hipError_t e = gated_ready(&zeros);
-  unsigned char *h = static_cast<unsigned char *>(workspace) + gated_out_bytes(rows, D, R, x_dtype);
+  const GatedFwdPlan plan = gated_fwd_plan(rows, D, R, x_dtype);
+  if ((rc = gated_room(fn, workspace, ws_bytes, plan.total)) != RESLIM_OK) return rc;
+  unsigned char *h = static_cast<unsigned char *>(workspace) + plan.hidden_at;
   const GatedIn in = {x, w->w_in, x_scale, w->in_scale, w->b_in, nullptr, h, rows, D, R};
-  if (e == hipSuccess) e = gated_forward(in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = gated_forward(plan, in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
 }
 
@@ -183,12 +194,13 @@ extern "C" int reslim_gated_mlp_fwd_train(const void *x, const reslim_gated_mlp_
   int rc = gated_check(fn, w, gate, rows, D, R, x_dtype, {x, gu, h, y}, {});
   if (rc != RESLIM_OK) return rc;
   if (x_dtype == RESLIM_E4M3) return refuse(RESLIM_EINVAL, fn, "training takes RESLIM_F32 or RESLIM_BF16");
-  if ((rc = gated_room(fn, workspace, ws_bytes, gated_fwd_bytes(rows, D, R, x_dtype))) != RESLIM_OK) return rc;
   if (rows == 0) return RESLIM_OK;
   const float *zeros = nullptr;
   hipError_t e = gated_ready(&zeros);
+  const GatedFwdPlan plan = gated_fwd_plan(rows, D, R, x_dtype);
+  if ((rc = gated_room(fn, workspace, ws_bytes, plan.total)) != RESLIM_OK) return rc;
   const GatedIn in = {x, w->w_in, nullptr, nullptr, w->b_in, gu, h, rows, D, R};
-  if (e == hipSuccess) e = gated_forward(in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = gated_forward(plan, in, w, x_dtype, gate == RESLIM_GATE_GELU, y, workspace, zeros, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
 }
 
@@ -242,11 +254,10 @@ extern "C" int reslim_gated_mlp_bwd(const void *x, const void *gu, const void *h
     if (e == hipSuccess) e = launch_gated_f32_wgrad(f(dy), f(h), o(grads->w_out), o(grads->b_out), rows, D, R, ws.wgrad, st);
     return e == hipSuccess ? RESLIM_OK : refuse_hip(fn, e);
   }
-  const GatedBwdPlan plan = gated_bwd_plan(rows, D, R);
   e = launch_gated_transpose(w->w_in, dx ? ws.wt_in : nullptr, w->w_out, ws.wt_out, D, R, st);
-  if (e == hipSuccess) e = launch_gated_dgate(plan.dgate, dy, ws.wt_out ? ws.wt_out : w->w_out, !ws.wt_out, gu, ws.d_gu, rows, D, R, gelu, st);
+  if (e == hipSuccess) e = launch_gated_dgate(ws.plan.dgate, dy, ws.wt_out ? ws.wt_out : w->w_out, !ws.wt_out, gu, ws.d_gu, rows, D, R, gelu, st);
   if (e == hipSuccess && dx)
-    e = launch_gated_out(plan.dx, ws.d_gu, ws.wt_in ? ws.wt_in : w->w_in, !ws.wt_in, nullptr, zeros, dx, rows, D, 2 * R, static_cast<float *>(ws.part), st);
+    e = launch_gated_out(ws.plan.dx, ws.d_gu, ws.wt_in ? ws.wt_in : w->w_in, !ws.wt_in, nullptr, zeros, dx, rows, D, 2 * R, static_cast<float *>(ws.part), st);
   if (e == hipSuccess) {
     WgradOp op[2];
     gated_ops(op, ws.d_gu, x, dy, h, D, R);

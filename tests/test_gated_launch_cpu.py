@@ -87,3 +87,28 @@ def test_the_planned_kernels_are_launched(plan, tmp_path_factory):
     for what, met in kinds.items():      # whole products of every kernel, slices, and rows of a last round
         assert {(RING, True, 1, RING), (SMALL, True, 1, SMALL), (SMALL, False, 1, SMALL), (WIDE, False, 1, WIDE), (TALL, False, 1, TALL)} <= met, (what, met)
         assert any(n == 2 for _, _, n, _ in met), (what, met)
+
+
+UNITS = """
+s.stand_in(512, 0, 0)                                   # the process meets a device of 512 compute units in this call
+out.append(lib.reslim_gated_mlp_fwd(p, None, gated_weights(), 0, *size, 1, p, p, small, None) if train == 0 else
+           lib.reslim_gated_mlp_fwd_train(p, gated_weights(), 0, *size, 1, p, p, p, p, small, None))
+out.append(launches())
+n = C.c_size_t(0)
+out.append(lib.reslim_gated_mlp_workspace_bytes(*size, 1, C.byref(n)))
+out.append(n.value)
+out.append(lib.reslim_gated_mlp_fwd(p, None, gated_weights(), 0, *size, 1, p, p, n.value, None))
+out.append(len(launches()))
+out.append(lib.reslim_gated_mlp_fwd(p, None, gated_weights(), 0, *size, 1, p, p, n.value - 1, None))
+out.append(len(launches()))
+"""
+
+
+@pytest.mark.parametrize("train", [0, 1])
+def test_a_workspace_is_checked_for_the_device_that_the_call_meets(tmp_path_factory, train):
+    """Twice the compute units, more slices of the output map: the size that was right for 256 is refused, before anything is enqueued."""
+    M, D, R = size = (128, 1024, 8192)
+    with_256 = ask(tmp_path_factory, "n = C.c_size_t(0)\nlib.reslim_gated_mlp_workspace_bytes(*size, 1, C.byref(n))\nout.append(n.value)", size=size)[0]
+    refused, nothing, ok, need, ran, launches, short, none = ask(tmp_path_factory, UNITS, size=size, small=with_256, train=train)
+    assert need > with_256
+    assert refused == -5 and nothing == [] and ok == 0 and ran == 0 and launches == 3 and short == -5 and none == 0
