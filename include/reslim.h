@@ -659,7 +659,8 @@ typedef struct {
 } reslim_gated_mlp_weights;
 
 /* y act [rows, D] from x x_dtype [rows, D] (x_scale: RESLIM_E4M3 only, else NULL).  The hidden layer is rounded to act
- * between the two products.  y must not alias an input. */
+ * between the two products.  y must not alias an input.  Workspaces of the BF16 and E4M3 forms go by the current device's compute units; a query
+ * without a device (no driver, no GPU) answers for the 256 of a whole MI355X. */
 int reslim_gated_mlp_workspace_bytes(int32_t rows, int32_t D, int32_t R, int32_t x_dtype, size_t *out);
 int reslim_gated_mlp_fwd(const void *x, const float *x_scale, const reslim_gated_mlp_weights *w, int32_t gate, int32_t rows,
                          int32_t D, int32_t R, int32_t x_dtype, void *y, void *workspace, size_t ws_bytes, void *hip_stream);

@@ -40,6 +40,13 @@ static hipError_t gated_ready(const float **zeros) {
   return hipSuccess;
 }
 
+// Workspaces of the bf16 and e4m3 forms go by the device's compute units; without a device they are sized for the 256 of a whole MI355X.
+static int gated_units(const char *fn, int x_dtype) {
+  const float *zeros = nullptr;
+  const hipError_t e = x_dtype == RESLIM_F32 ? hipSuccess : gated_ready(&zeros);
+  return e == hipSuccess || e == hipErrorNoDevice ? RESLIM_OK : refuse_hip(fn, e);
+}
+
 // ------------------------------------------------------------------ no rows: parameter gradients of zero
 struct ZeroArgs { uint16_t *p[4]; int64_t n[4]; };
 __global__ __launch_bounds__(256) void gated_zero_kernel(ZeroArgs a) {
@@ -162,10 +169,9 @@ using namespace reslim;
 extern "C" int reslim_gated_mlp_workspace_bytes(int32_t rows, int32_t D, int32_t R, int32_t x_dtype, size_t *out) {
   const char *fn = "reslim_gated_mlp_workspace_bytes";
   if (!out) return refuse(RESLIM_EINVAL, fn, "null argument");
-  const int rc = gated_shape(fn, rows, D, R, x_dtype);
+  int rc = gated_shape(fn, rows, D, R, x_dtype);
   if (rc != RESLIM_OK) return rc;
-  const float *zeros = nullptr;
-  if (x_dtype != RESLIM_F32) (void)gated_ready(&zeros);      // the slices go by the device's compute units
+  if ((rc = gated_units(fn, x_dtype)) != RESLIM_OK) return rc;
   *out = gated_fwd_plan(rows, D, R, x_dtype).total;
   return RESLIM_OK;
 }
@@ -215,9 +221,8 @@ extern "C" int reslim_gated_mlp_bwd_workspace_bytes(int32_t rows, int32_t D, int
   if (!out) return refuse(RESLIM_EINVAL, fn, "null argument");
   int rc = gated_shape(fn, rows, D, R, x_dtype);
   if (rc == RESLIM_OK) rc = gated_grad_type(fn, x_dtype, grad_dtype);
+  if (rc == RESLIM_OK) rc = gated_units(fn, x_dtype);
   if (rc != RESLIM_OK) return rc;
-  const float *zeros = nullptr;
-  if (x_dtype == RESLIM_BF16) (void)gated_ready(&zeros);      // the slices go by the device's compute units
   *out = plan_gated_bwd(rows, D, R, x_dtype, nullptr).total;
   return RESLIM_OK;
 }

@@ -112,3 +112,19 @@ def test_a_workspace_is_checked_for_the_device_that_the_call_meets(tmp_path_fact
     refused, nothing, ok, need, ran, launches, short, none = ask(tmp_path_factory, UNITS, size=size, small=with_256, train=train)
     assert need > with_256
     assert refused == -5 and nothing == [] and ok == 0 and ran == 0 and launches == 3 and short == -5 and none == 0
+
+
+@pytest.mark.parametrize("device,attribute,code", [(100, 0, 0), (1, 0, -4), (0, 1, -4)], ids=["no device", "device error", "attribute error"])
+def test_workspace_queries_report_errors(tmp_path_factory, device, attribute, code):
+    """Without a device the sizes are those of 256 compute units; any other error is the call's."""
+    got = ask(tmp_path_factory, """
+s.stand_in(64, device, attribute)
+for query in (lambda n: lib.reslim_gated_mlp_workspace_bytes(128, 1024, 8192, 1, n), lambda n: lib.reslim_gated_mlp_bwd_workspace_bytes(128, 1024, 8192, 1, 1, n)):
+    n = C.c_size_t(0)
+    out.append([query(C.byref(n)), n.value, lib.reslim_last_error(None).decode() if want else ""])
+out.append([lib.reslim_gated_mlp_workspace_bytes(128, 1024, 8192, 0, C.byref(n)), n.value, ""])      # fp32 asks no device
+""", device=device, attribute=attribute, want=code)
+    assert [g[0] for g in got] == [code, code, 0]
+    assert all((g[1] > 0) == (g[0] == 0) for g in got)
+    if code:
+        assert all("workspace_bytes" in g[2] for g in got[:2])
