@@ -128,3 +128,21 @@ out.append([lib.reslim_gated_mlp_workspace_bytes(128, 1024, 8192, 0, C.byref(n))
     assert all((g[1] > 0) == (g[0] == 0) for g in got)
     if code:
         assert all("workspace_bytes" in g[2] for g in got[:2])
+
+
+def test_the_gpu_tests_of_few_fp32_rows_take_their_kernel(tmp_path_factory):
+    text = open(os.path.join(os.path.dirname(os.path.abspath(__file__)), "test_gpu_gated_few_rows.py")).read()
+    sizes, taken = (eval(re.search(r"^%s = (.*)$" % n, text, re.M).group(1)) for n in ("SIZES", "TAKEN"))
+    got = ask(tmp_path_factory, """
+for size in sizes:
+    out.append([lib.reslim_gated_mlp_fwd(p, None, gated_weights(), gate, *size, 0, p, p, 1 << 40, None) for gate in (0, 1)])
+    out.append([k for k, _ in launches() if "sum" not in k])
+""", sizes=sizes)
+    for size, want, rc, kernels in zip(sizes, taken, got[::2], got[1::2]):
+        assert rc == [0, 0] and len(kernels) == 4
+        for k, gelu in ((0, "false"), (2, "true")):
+            assert tuple("gated_f32_few_kernel" in n for n in kernels[k:k + 2]) == want, (size, kernels)
+            assert not want[0] or f"<2, {gelu}>" in kernels[k], kernels
+            assert not want[1] or "<1, false>" in kernels[k + 1], kernels
+    steps = {(k // 16 + 7) // 8 for s, t in zip(sizes, taken) for k, on in zip((s[1], s[2]), t) if on}
+    assert {1, 2, 4, 5, 8, 17, 22} <= steps, steps      # steps a wave: fewer than, as many as and more than the four of a turn and the eight of two
