@@ -98,13 +98,14 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
     // the largest magnitude of the row becomes 448; a row of zeros keeps scale 0 and zeros
     top = row_all<NT, true>(top, box[1]);
     if (t == 0) a.y_scale[row] = top / kE4m3Max;
-    const float up = top > 0.f ? fminf(kE4m3Max / top, 3.402823466e+38f) : 0.f;
+    const float lift = top < 0x1p-96f ? 0x1p64f : 1.0f;      // 448 / top leaves fp32 below 2^-119
+    const float up = top > 0.f ? kE4m3Max / (top * lift) : 0.f;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int k = (i * NT + t) * V;
       if (k < a.D) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j] *= up;
+        for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * lift * up;
         store(static_cast<e4m3_t *>(a.y) + at, k, v[i]);
       }
     }

@@ -262,3 +262,20 @@ def test_binding_refuses():
             B.reslim_rmsnorm_fwd(a["x"], a["gamma"], a["y"], delta=a["delta"], sum_out=a["sum_out"])
     with pytest.raises(B.ReslimError):
         B.reslim_rmsnorm_fwd(x, gamma, torch.empty(4, 64, dtype=Q, device="cuda"))      # no y_scale
+
+
+@pytest.mark.parametrize("D", [48, 513, 4096])
+@pytest.mark.parametrize("size", [1.0, 1e-30, 1e-35, 1e-36, 1e-37, 1e-38, 1e-40, 1e-42])
+def test_e4m3_of_rows_at_the_end_of_fp32(size, D):
+    """Rows whose largest magnitude is too small for 448 / max: they still span the 8-bit range."""
+    x = torch.randn(5, D, generator=torch.Generator(device="cuda").manual_seed(D), device="cuda")
+    gamma = torch.full((D,), size, device="cuda")
+    y, scale = torch.empty(5, D, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(5, device="cuda")
+    B.reslim_rmsnorm_fwd(x, gamma, y, y_scale=scale)
+    _, want = P.rmsnorm(x, None, gamma, 1e-6)
+    top = want.abs().amax(1, keepdim=True)
+    assert bool((y.float().abs().amax(1) == 448).all())
+    # y gamma rounded among fp32's subnormal values, 2^-150; half a step of e4m3, 2^-4 of the value or 2^-10 of the scale; a scale among the subnormal values is off by
+    # up to 2^-150, 448 times that at the top; the norm's sums and products some 40 half steps of fp32
+    bound = want.abs() * (2.0 ** -4 + 64 * P.E) + top / 448 * 2.0 ** -10 + 450 * 2.0 ** -150
+    assert P.worst(y.double() * scale.double()[:, None], want, bound * 1.01) <= 1
