@@ -146,3 +146,19 @@ for size in sizes:
             assert not want[1] or "<1, false>" in kernels[k + 1], kernels
     steps = {(k // 16 + 7) // 8 for s, t in zip(sizes, taken) for k, on in zip((s[1], s[2]), t) if on}
     assert {1, 2, 4, 5, 8, 17, 22} <= steps, steps      # steps a wave: fewer than, as many as and more than the four of a turn and the eight of two
+
+
+def test_the_gpu_tests_of_cut_products_cut_them(tmp_path_factory):
+    """In the whole calls the product is cut behind row 16,384, with each kernel for the rest; the parts are cut elsewhere or not at all, and none is sliced."""
+    text = open(os.path.join(os.path.dirname(os.path.abspath(__file__)), "test_gpu_gated_cuts.py")).read()
+    given = {"AT": 16384}
+    for n in ("AT", "ROWS", "PARTS"):
+        given[n] = eval(re.search(r"^%s = (.*?)(  #.*)?$" % n, text, re.M).group(1), {}, given)
+    for what, R in (("out", 2048), ("dx", 1024)):
+        calls = [(rows, None) for rows in given["ROWS"]] + [(rows, p) for rows in given["ROWS"] for p in given["PARTS"]]
+        sizes = [(rows if p is None else len(range(rows)[slice(*p)]), 2048, R) for rows, p in calls]
+        found = [_products(fwd if what == "out" else bwd) for _, fwd, bwd in ask(tmp_path_factory, CALLS, sizes=sizes)]
+        assert found[:3] == [[(WIDE, 1), (k, 1)] for k in (RING, SMALL, TALL)], (what, found[:3])
+        assert all(s == 1 for f in found for _, s in f), (what, found)
+        whole = {k for f in found[3:] if len(f) == 1 for k, _ in f}
+        assert {SMALL, WIDE, TALL} & whole == whole and len(whole) >= 2, (what, whole)
