@@ -26,7 +26,7 @@ struct F32Args {
   float *out, *keep;                   // keep: kGate, [gate | up] or null
   int M, N, K;                         // kGate, kDGate: N features, with 2 N columns of gu
   int64_t a_step, b_step;              // elements from row to row (k contiguous) or from k to k (rows contiguous)
-  int k_per;                           // k of a slice, a multiple of 16
+  int k_per;                           // k of a slice, a multiple of kBK
   int64_t slice;                       // floats between the slices' results
   float *sums;                         // kPlain with A read across: sums over k of A's rows [slices, M], or null
 };

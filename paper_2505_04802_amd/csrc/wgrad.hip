@@ -520,7 +520,7 @@ static hipError_t launch_wgrad_bf16(const WgradPlan &p, const WgradOp *op, int n
 }
 
 // for each layer dW[N, K] = dY[M, N]^T X[M, K] and db[N] = column sums of dY, both fp32; ws as sized by wgrad_ws_bytes
-// (rounded: bf16 operands, gradients rounded to bf16; ws as sized by wgrad_rounded_ws_bytes)
+// (rounded: bf16 operands, dw and db point at bf16 and get the sums rounded once)
 hipError_t launch_wgrad(int dtype, const WgradOp *op, int n_op, int M, void *ws, hipStream_t st, bool rounded) {
   if (rounded && dtype != RESLIM_BF16) return hipErrorInvalidValue;
   if (M <= 0 || n_op < 1 || n_op > kWgradMax) return hipErrorInvalidValue;

@@ -185,3 +185,15 @@ def test_binding_refuses():
             B.reslim_rotary_fwd(a["x"], a["out"], a["pos"], a["freq"], heads=a["heads"])
     with pytest.raises(B.ReslimError):
         B.reslim_rotary_fwd(x, x[:, :4].contiguous(), pos, _table(128, 1)[0], heads=4)      # more features than a head has
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [H, F], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dh,rot", [(70, 64), (66, 32), (18, 16), (130, 128)])
+def test_in_place_beside_features_that_end_inside_a_piece(dh, rot, dtype, layout):
+    freq, _ = _table(rot, 1)
+    pos, x = _positions(1, 37), _x(37, 7, dh, dtype)
+    y = x.clone()
+    B.reslim_rotary_fwd(y, y, pos, freq, heads=5, layout=layout)
+    _check(x, y[:, :5], pos, freq, 5, layout, 1.0)
+    assert torch.equal(y[:, 5:], x[:, 5:])
