@@ -162,3 +162,18 @@ def test_the_gpu_tests_of_cut_products_cut_them(tmp_path_factory):
         assert all(s == 1 for f in found for _, s in f), (what, found)
         whole = {k for f in found[3:] if len(f) == 1 for k, _ in f}
         assert {SMALL, WIDE, TALL} & whole == whole and len(whole) >= 2, (what, whole)
+
+
+def test_the_gpu_tests_of_short_contractions_take_the_large_kernels(tmp_path_factory):
+    text = open(os.path.join(os.path.dirname(os.path.abspath(__file__)), "test_gpu_gated_slabs.py")).read()
+    e4m3, bf16 = (eval(re.search(r"^%s = (\[.*?\])" % n, text, re.M).group(1)) for n in ("E4M3", "BF16"))
+    got = ask(tmp_path_factory, """
+for size in e4m3:
+    lib.reslim_gated_mlp_fwd(p, p, gated_weights(in_scale=p), 0, *size, 2, p, p, 1 << 40, None)
+    out.append(launches()[0][0])
+for size in bf16:
+    lib.reslim_gated_mlp_bwd(p, p, p, p, gated_weights(), 0, *size, 1, 1, p, GRADS, p, 1 << 40, None)
+    out.append([k for k, _ in launches() if ", 64>" in k or "<64, true>" in k][0])      # the hidden layer's gradient
+""", e4m3=e4m3, bf16=bf16)
+    assert ["gemm_bf16_pp_kernel<2, 36>" in got[0], "gemm_bf16_pp_kernel<2, 36>" in got[1], "gemm_bf16_pp_kernel<1, 36>" in got[2]] == [True] * 3, got
+    assert all("gemm_bf16_kernel<128, 128" in k for k in got[4:6]) and "gemm_bf16_pp_kernel<2, 64>" in got[-1], got
