@@ -572,7 +572,7 @@ int reslim_asc_forward(reslim_ctx *ctx, const reslim_asc_plan *plan, const float
  * around tiles_attention_fwd, and its gradient.  No context is needed; sizes come with the call.  All pointers are device
  * pointers on the current device unless stated; tensors are contiguous row-major unless a stride is given; work is enqueued
  * on hip_stream, nothing is allocated or synchronised, and calls with buffers of their own may overlap.  Results are
- * deterministic.  Sums, statistics and products are fp32 (angles 64-bit), results are rounded once.  rows = 0 (tokens = 0)
+ * deterministic.  Sums, statistics and products are fp32 (angles 64-bit), results are rounded once; what else is rounded on the way is said.  rows = 0 (tokens = 0)
  * is allowed: nothing is written but parameter gradients, which become zero.  Outputs must not overlap inputs or each other
  * but where "in place" is said.  A refusal enqueues nothing; its text is at
  * reslim_last_error(NULL).  Errors: RESLIM_EINVAL (null, type, alignment, value), RESLIM_ESHAPE, RESLIM_EWORKSPACE (null,
@@ -647,7 +647,7 @@ int reslim_rotary_frequencies(int32_t rot, int32_t axes, double base, int32_t sc
  * Types: x_dtype F32 (act float), BF16 (act bfloat16) or E4M3 (act bfloat16; forward only): x rows with x_scale float [rows] as
  * reslim_rmsnorm_fwd writes them.  rows <= 2,000,000,000, D <= 16384, R <= 65536; BF16: D and R multiples of 64, E4M3: D of 128, R of 64; F32: any
  * sizes, rows <= 4,000,000 and at most 2^23 tiles of 64 rows by 32 of R, or 64 of D.  BF16 and E4M3 buffers start on 16 bytes.
- * With act bfloat16 GELU is good to 1.5e-5 of its value, below -5 to 1.6e-3, and 0 below -14.  act(+inf) = inf; act(-inf) and act' at either infinity are
+ * With act bfloat16 GELU is good to 1.5e-5 of its value, below -5 to 1.6e-3, and 0 below -14; with act float to a few 2^-24 |g|.  act(+inf) = inf; act(-inf) and act' at either infinity are
  * NaN, as the formulas g / (1 + e^-g) and g Phi(g) and their derivatives give in fp32. */
 enum { RESLIM_GATE_SILU = 0, RESLIM_GATE_GELU = 1 };
 typedef struct {

@@ -5,8 +5,8 @@
 // the gate projection of 32 features in its column half 0 and the up projection of the same features in column half 1.  The
 // hidden layer is then formed in the accumulators and written once, M R values instead of 2 M R written and read again.
 //   Large products are bound by the matrix instructions at the power limit: 37,520 x 4096 x 2 x 10,944 in e4m3 2.44 ms, 2760 TFLOP/s (the library's
-// 8192^3 2809); 80,704 x 1024 x 2 x 2752 in bf16 with [gate | up] kept 0.87-0.90 ms, 1020 TFLOP/s (library 1462), where a tile has 16 slabs to 10 us
-// of epilogue.  Few rows are bound by memory: see the 64 x 64 tiles.
+// 8192^3 2809); 80,704 x 1024 x 2 x 2752 in bf16 with [gate | up] kept 0.87-1.05 ms, 870-1050 TFLOP/s, where a tile has 16 slabs to 10 us
+// of epilogue (the library's product of that shape alone 0.78-0.80 ms).  Few rows are bound by memory: see the 64 x 64 tiles.
 #include <algorithm>
 #include <type_traits>
 
@@ -124,7 +124,7 @@ __device__ __forceinline__ void gate_gradient(float dh, uint32_t gates, uint32_t
 // LDS (row r at 128 r bytes, its 16-byte chunk c at c ^ ((r >> 1) & 7)), so that eight lanes hold 32 neighbouring columns of a row
 // and read and write 64-byte segments.  The kept values come from memory while nothing else of the wave runs, so their loads go out as
 // far ahead as registers allow: FIRST blocks before the first one, and for every block that has left the accumulators two more.  40,352 x 1024 x
-// 2752 takes 350 us (650 TFLOP/s, 0.89 GB of gate, up and gradients): 255 without the reads, 240 without reads and stores.
+// 2752 takes 343-367 us (620-660 TFLOP/s, 0.89 GB of gate, up and gradients; the library's product of that shape alone 242): 255 without the reads, 240 without reads and stores.
 template <int EPI, bool GUARD, int MI, int NI>
 __device__ __forceinline__ void epilogue_dgate(const GemmArgs &g, const f32x16 (&acc)[MI][NI], int m_base, int n_base, int lane, unsigned char *stg) {
   constexpr bool kGelu = EPI & kEpiGelu1;
