@@ -22,7 +22,6 @@ extern "C" int choose(int M, int N, int slabs, int sliceable, double other, int 
 extern "C" int whole(int M, int N, int slabs) { return gated_whole_rounds(M, N, slabs, kEpiAct, 256); }
 """
 RING, SMALL, WIDE, TALL = 1, 2, 3, 4
-BF16 = 1
 CALLS = """
 for M, D, R in sizes:
     rc = [lib.reslim_gated_mlp_fwd(p, None, gated_weights(), 0, M, D, R, 1, p, p, 1 << 40, None)]
